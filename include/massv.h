@@ -135,6 +135,31 @@ int massv_verify_attn(const massv_attn_desc *desc, const void *q, const void *k_
                       void *out, float *out_f32, float *lse,
                       void *workspace, size_t workspace_bytes, int32_t *dev_status, massv_stream_t stream);
 
+/* Bytes of scratch massv_verify_attn_shared needs for this geometry and number of groups (0 on a bad descriptor or one it does not support). */
+size_t massv_verify_attn_shared_workspace_size(const massv_attn_desc *desc, int32_t n_groups);
+
+/*
+ * massv_verify_attn for sequences whose contexts begin with the same positions: several questions about one image, several
+ * samples of one prompt.  The result is that of massv_verify_attn on the same arguments (append included); the shared positions
+ * are read and multiplied once per group instead of once per sequence.
+ *
+ *   n_groups        1 .. 256
+ *   group_start     int32 [n_groups + 1], 0 = group_start[0] <= ... <= group_start[n_groups] = B: group g is the sequences
+ *                   group_start[g] .. group_start[g + 1] - 1.  Anything else stores MASSV_ERR_INVALID_ARG in dev_status, and nothing is shared.
+ *   shared_lens     int32 [n_groups]: the first shared_lens[g] positions are the same for all sequences of group g, i.e. their
+ *                   page tables have the same page ids for every page that lies wholly inside them.  More than a
+ *                   member has committed is taken as the least of the members' lengths.  The ids are read from the group's first sequence.
+ *   other arguments as for massv_verify_attn; desc->window must be 0 (MASSV_ERR_UNSUPPORTED otherwise: a local layer reads only
+ *                   its window, with massv_verify_attn on the same page tables)
+ * A group of one sequence, and what a group shares beyond whole blocks of 128 positions, are read per sequence.  A
+ * sequence whose lengths violate the capacity rule is skipped, as in massv_verify_attn, and does not count as a member.
+ */
+int massv_verify_attn_shared(const massv_attn_desc *desc, int32_t n_groups, const int32_t *group_start, const int32_t *shared_lens,
+                             const void *q, const void *k_new, const void *v_new,
+                             void *k_pages, void *v_pages, const int32_t *page_table, const int32_t *seq_lens,
+                             void *out, float *out_f32, float *lse,
+                             void *workspace, size_t workspace_bytes, int32_t *dev_status, massv_stream_t stream);
+
 /* Bytes of scratch massv_accept needs (0 on a bad descriptor).  Includes room
  * for the fp32 logits when T > 0, whether or not logits_out is supplied. */
 size_t massv_accept_workspace_size(const massv_accept_desc *desc);
@@ -307,6 +332,139 @@ int massv_tvd_histogram(int64_t n, const float *tvd, int32_t bins, int64_t *coun
 int massv_sample_top_p(int32_t rows, int32_t vocab, float temperature, float top_p, const float *logits,
                        const float *u, int32_t *tokens, float *probs_out, int32_t *dev_status,
                        massv_stream_t stream);
+
+/*
+ * Rotary positions.  massv_verify_attn takes queries and keys with their positional encoding applied; this is the encoding that
+ * the paper's target models use (Sec. 4 "Models"), for the block rows of a step and for prompts.
+ *
+ * A head's first rot_dim elements form rot_dim / 2 pairs: (i, i + rot_dim / 2) in the HALF layout, (2 i, 2 i + 1) in the
+ * INTERLEAVED one; the elements behind them are copied.  Pair i of a token at position p turns by the angle p * f_i:
+ *     (x, y) -> magnitude * (x cos - y sin, x sin + y cos).
+ * With several position axes (an image's tokens have a time, a row and a column), the first axis_pairs[0] pairs take the
+ * position on axis 0, the next axis_pairs[1] that on axis 1, and so on.
+ */
+#define MASSV_ROPE_HALF 0
+#define MASSV_ROPE_INTERLEAVED 1
+#define MASSV_ROPE_BACKWARD 1u           /* flags: the transposed map (angles negated), which takes the gradient of the outputs to that of the inputs, and undoes the map where magnitude is 1 */
+
+typedef struct massv_rope_desc {
+    int32_t batch;               /* B >= 1 */
+    int32_t rows;                /* tokens per sequence >= 1; B * rows <= 2^31 - 1 */
+    int32_t n_q_heads;           /* heads of q; 0: no q */
+    int32_t n_kv_heads;          /* heads of k; 0: no k */
+    int32_t head_dim;            /* d: a multiple of 8, 8 .. 256 */
+    int32_t rot_dim;             /* elements that turn: even, 2 .. d */
+    int32_t layout;              /* MASSV_ROPE_HALF or MASSV_ROPE_INTERLEAVED */
+    int32_t n_axes;              /* position components of a token: 1 .. 3 */
+    int32_t axis_pairs[3];       /* pairs that follow each axis; their sum is rot_dim / 2 */
+    float magnitude;             /* factor on the turned elements (some long-context scalings have one); 1 = none */
+    uint32_t flags;              /* 0 or MASSV_ROPE_BACKWARD */
+} massv_rope_desc;
+
+/* How the frequencies are stretched for contexts longer than those of training.  Unscaled: f_i = base^(-2 i / rot_dim). */
+#define MASSV_ROPE_SCALE_NONE 0
+#define MASSV_ROPE_SCALE_LINEAR 1        /* f_i / factor */
+#define MASSV_ROPE_SCALE_BASE 2          /* the base times factor^(rot_dim / (rot_dim - 2)): the slowest pair is divided by factor, the fastest kept (rot_dim > 2) */
+#define MASSV_ROPE_SCALE_TURNS 3         /* f_i (w + (1 - w) / factor), w rising linearly from 0 to 1 as the turns over original_context, original_context * f_i / (2 pi), go from slow to fast */
+#define MASSV_ROPE_SCALE_PAIRS 4         /* the same with w falling linearly in the pair's index, from 1 at floor(index(fast)) to 0 at ceil(index(slow)) (both clamped to 0 .. rot_dim - 1);
+                                            index(t) = rot_dim ln(original_context / (2 pi t)) / (2 ln base) is where a pair makes t turns */
+#define MASSV_ROPE_SCALE_GIVEN 5         /* inv_freq[i], radians per position */
+
+typedef struct massv_rope_scaling {
+    int32_t kind;                /* MASSV_ROPE_SCALE_* */
+    double factor;               /* >= 1 (LINEAR, BASE, TURNS, PAIRS) */
+    double original_context;     /* > 0 (TURNS, PAIRS) */
+    double slow, fast;           /* 0 < slow < fast (TURNS, PAIRS) */
+    const double *inv_freq;      /* HOST array of rot_dim / 2 values (GIVEN) */
+} massv_rope_scaling;
+
+/*
+ * Host only: the frequencies in the form massv_rotary takes, turns per position as a 64-bit fraction (f_i / (2 pi) mod 1, times
+ * 2^64), into the HOST array turns[rot_dim / 2].  The product with a position then wraps where the angle does, so that an angle is
+ * as exact at position 10^9 as at 1.  scaling NULL: none.  base > 1 (not read with GIVEN).
+ */
+int massv_rope_frequencies(int32_t rot_dim, double base, const massv_rope_scaling *scaling, uint64_t *turns);
+
+/*
+ * Turns q and k by their positions.  Token t = b * rows + j; its position is
+ *   positions[t * n_axes + axis]                                  where positions is given, else
+ *   seq_lens[b] + j + (pos_delta ? pos_delta[b] : 0) on every axis  (a block at the end of its context, without a host round trip;
+ *                                                                 pos_delta for image tokens that share positions).
+ *   turns          uint64 [rot_dim / 2] (device copy of massv_rope_frequencies' result)
+ *   q, q_out       bf16; token t's heads are n_q_heads * d consecutive elements from t * stride on (strides in elements, multiples
+ *                  of 8, at least n_q_heads * d): a slice of a fused projection's output is taken as it is, and packed on the way out.
+ *                  q_out may be q (same stride); otherwise the two do not overlap.  k, k_out alike.
+ *   positions      int32 [B * rows, n_axes] or NULL;  seq_lens int32 [B] or NULL (one of the two);  pos_delta int32 [B] or NULL
+ * Math: angles exact to 2^-62 of a turn, sine and cosine and products in fp32, one rounding to bf16.  No workspace.
+ */
+int massv_rotary(const massv_rope_desc *desc, const uint64_t *turns, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                 const int32_t *positions, const int32_t *seq_lens, const int32_t *pos_delta,
+                 void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, massv_stream_t stream);
+
+/*
+ * Rules that a request puts on its logits, ahead of the softmax of massv_accept and massv_sample_top_p (which take the logits as
+ * the model gives them).  Every array is optional (NULL: the rule is off) and lives on the device; V = vocab, W = ceil(V / 32).
+ * The logit z of token v in row j of sequence b becomes, in this order, each operation rounded to fp32:
+ *   1. z + bias                     of the last entry k of bias_start[b] .. bias_start[b + 1] - 1 with bias_tokens[k] == v
+ *   2. z / r (z > 0), z * r (else)  where the token was seen: in the prompt (prompt_bits) or in the output (c > 0)
+ *   3. z - frequency[b] * c        where c > 0
+ *   4. z - presence[b]              where c > 0
+ *   5. -inf                         where the row's bit in `allowed` is 0 (whatever z is, NaN too)
+ * with r = repetition[b] and c = counts[b, v] + the number of drafts i < j equal to v: in a speculative block, row j follows
+ * the drafts ahead of it.
+ */
+typedef struct massv_logit_rules {
+    const uint32_t *allowed;      /* [B, R, W]: bit v % 32 of word v / 32 is 1 where the grammar allows token v */
+    const int32_t *bias_start;    /* [B + 1], the first entry of each sequence */
+    const int32_t *bias_tokens;   /* [n_bias] */
+    const float *bias_values;     /* [n_bias] */
+    int32_t n_bias;               /* entries in the two arrays */
+    const uint32_t *prompt_bits;  /* [B, W]: tokens of the prompt */
+    const uint32_t *output_bits;  /* [B, W]: tokens with a count; counts are read only where the bit is set */
+    const int32_t *counts;        /* [B, V]: occurrences in the output so far (with output_bits) */
+    const float *repetition;      /* [B], > 0 */
+    const float *frequency;       /* [B] */
+    const float *presence;        /* [B] */
+} massv_logit_rules;
+
+/*
+ * The rules alone, for the rows a drafter samples from or any others: batch sequences of gamma + 1 rows.
+ *   logits, logits_out  fp32 [B, R, V]; may be the same buffer, otherwise they do not overlap
+ *   draft_tokens        int32 [B, gamma]; NULL: no drafts in the history
+ * 1 <= batch <= 65535, gamma 0 .. 7, 1 <= vocab <= 2^21.  Reads the logits of allowed tokens once; in place, writes only what changes.
+ * A bias entry whose token is outside [0, V) or whose index is outside [0, n_bias), and a repetition that is not > 0, are
+ * ignored and store MASSV_ERR_INVALID_ARG in dev_status.  Drafts outside [0, V) are ignored.  No workspace.
+ */
+int massv_logits_apply(int32_t batch, int32_t gamma, int32_t vocab, const massv_logit_rules *rules, const float *logits,
+                       float *logits_out, const int32_t *draft_tokens, int32_t *dev_status, massv_stream_t stream);
+
+/* Bytes of scratch massv_accept_logits needs (0 on a bad descriptor). */
+size_t massv_accept_logits_workspace_size(const massv_accept_desc *desc);
+
+/*
+ * massv_accept from logits that are there already (for instance those of massv_shard_lm_head with one rank), under rules: the
+ * rows' softmax statistics are made in the pass that applies the rules.
+ *   desc          as for massv_accept; `hidden` is not read
+ *   rules         NULL: none (logits_out is not used then)
+ *   logits        fp32 [B, R, V]
+ *   logits_out    the logits under the rules; may be the buffer of logits.  Required with rules at T > 0, optional at T == 0.
+ *   other arguments as for massv_accept (probs_out: the distribution under the rules)
+ * A row of which the rules leave nothing yields token 0 and MASSV_ERR_INVALID_ARG, as in massv_accept.
+ */
+int massv_accept_logits(const massv_accept_desc *desc, const massv_logit_rules *rules, const float *logits, float *logits_out,
+                        const int32_t *draft_tokens, const float *draft_probs, const float *u_accept, const float *u_sample,
+                        int32_t *out_tokens, int32_t *accept_len, float *probs_out,
+                        void *workspace, size_t workspace_bytes, int32_t *dev_status, massv_stream_t stream);
+
+/*
+ * Adds tokens to a history: sets their bits and, where counts is given, counts them.  tokens int32 [B, n_max], of which the first
+ * lens[b] count (lens NULL: all n_max).  With out_tokens, gamma + 1 and accept_len of an acceptance call it takes a step's
+ * result into output_bits and counts; with prompts and counts NULL it fills prompt_bits.  Tokens outside [0, V) and lengths outside
+ * [0, n_max] (taken as the nearest bound) store MASSV_ERR_INVALID_ARG.  bits uint32 [B, W], counts int32 [B, V], zeroed by the
+ * caller at a request's start.  n_max >= 0; no workspace.
+ */
+int massv_history_add(int32_t batch, int32_t vocab, const int32_t *tokens, int32_t n_max, const int32_t *lens,
+                      uint32_t *bits, int32_t *counts, int32_t *dev_status, massv_stream_t stream);
 
 /*
  * Acceptance with the vocabulary cut across `world` ranks (tensor-parallel LM head).  The arithmetic is

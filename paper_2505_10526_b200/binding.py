@@ -41,6 +41,24 @@ class AcceptDesc(ctypes.Structure):
                 ("vocab", ctypes.c_int32), ("temperature", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("rows", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("axis_pairs", ctypes.c_int32 * 3), ("magnitude", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class _RopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double), ("original_context", ctypes.c_double), ("slow", ctypes.c_double),
+                ("fast", ctypes.c_double), ("inv_freq", ctypes.POINTER(ctypes.c_double))]
+
+
+class LogitRules(ctypes.Structure):
+    """The rules of massv_logits_apply / massv_accept_logits (``logit_rules`` makes one and keeps its tensors alive)."""
+    _fields_ = [("allowed", ctypes.c_void_p), ("bias_start", ctypes.c_void_p), ("bias_tokens", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("n_bias", ctypes.c_int32), ("prompt_bits", ctypes.c_void_p), ("output_bits", ctypes.c_void_p), ("counts", ctypes.c_void_p),
+                ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python {os.path.join(_PKG, 'build.py')}` "
@@ -90,6 +108,25 @@ def _load():
     lib.massv_shard_set_token.argtypes = [D, i32, vp, i32p, i32p, i32p, vp]
     lib.massv_kv_commit.restype = ctypes.c_int
     lib.massv_kv_commit.argtypes = [ctypes.c_int32, ctypes.c_int32, i32p, i32p, i32p, vp]
+    lib.massv_rope_frequencies.restype = ctypes.c_int
+    lib.massv_rope_frequencies.argtypes = [i32, ctypes.c_double, ctypes.POINTER(_RopeScaling), ctypes.POINTER(ctypes.c_uint64)]
+    lib.massv_rotary.restype = ctypes.c_int
+    lib.massv_rotary.argtypes = [ctypes.POINTER(RopeDesc), vp, vp, ctypes.c_int64, vp, ctypes.c_int64, i32p, i32p, i32p, vp, ctypes.c_int64, vp,
+                                 ctypes.c_int64, vp]
+    lib.massv_verify_attn_shared_workspace_size.restype = ctypes.c_size_t
+    lib.massv_verify_attn_shared_workspace_size.argtypes = [ctypes.POINTER(AttnDesc), i32]
+    lib.massv_verify_attn_shared.restype = ctypes.c_int
+    lib.massv_verify_attn_shared.argtypes = [ctypes.POINTER(AttnDesc), i32, i32p, i32p, vp, vp, vp, vp, vp, i32p, i32p, vp, f32p, f32p, vp,
+                                             ctypes.c_size_t, i32p, vp]
+    rules = ctypes.POINTER(LogitRules)
+    lib.massv_logits_apply.restype = ctypes.c_int
+    lib.massv_logits_apply.argtypes = [i32, i32, i32, rules, f32p, f32p, i32p, i32p, vp]
+    lib.massv_accept_logits_workspace_size.restype = ctypes.c_size_t
+    lib.massv_accept_logits_workspace_size.argtypes = [D]
+    lib.massv_accept_logits.restype = ctypes.c_int
+    lib.massv_accept_logits.argtypes = [D, rules, f32p, f32p, i32p, f32p, f32p, f32p, i32p, i32p, f32p, vp, ctypes.c_size_t, i32p, vp]
+    lib.massv_history_add.restype = ctypes.c_int
+    lib.massv_history_add.argtypes = [i32, i32, i32p, i32, i32p, vp, i32p, i32p, vp]
     lib.massv_strerror.restype = ctypes.c_char_p
     lib.massv_strerror.argtypes = [ctypes.c_int]
     lib.massv_version.restype = ctypes.c_int
@@ -117,7 +154,9 @@ def _load_marshal():
                           f"`python {os.path.join(_PKG, 'build.py')}` (there is no fallback path)") from e
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
     _marshal.bind(address(_lib.massv_verify_attn), address(_lib.massv_accept), address(_lib.massv_kv_commit),
-                  address(_lib.massv_sample_top_p), address(_lib.massv_tvd), AttnDesc, AcceptDesc)
+                  address(_lib.massv_sample_top_p), address(_lib.massv_tvd), address(_lib.massv_rotary), address(_lib.massv_verify_attn_shared),
+                  address(_lib.massv_logits_apply), address(_lib.massv_accept_logits), address(_lib.massv_history_add),
+                  AttnDesc, AcceptDesc, RopeDesc, LogitRules)
     return _marshal
 
 
@@ -282,6 +321,103 @@ def massv_sample_top_p(logits, u, tokens, temperature, top_p, probs_out=None, de
     rc = _native.sample_top_p(rows, vocab, temperature, top_p, logits, u, tokens, probs_out, dev_status)
     if rc != 0:
         raise MassvError(rc, "massv_sample_top_p")
+
+
+# ---- rotary positions
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_TURNS, ROPE_SCALE_PAIRS, ROPE_SCALE_GIVEN = range(6)
+
+
+def rope_desc(batch, rows, n_q_heads, n_kv_heads, head_dim, rot_dim=None, layout=ROPE_HALF, axis_pairs=None, magnitude=1.0, backward=False) -> RopeDesc:
+    """``axis_pairs``: pairs that follow each of the 1 .. 3 position axes (default: one axis for all)."""
+    rot_dim = head_dim if rot_dim is None else rot_dim
+    pairs = [rot_dim // 2] if axis_pairs is None else list(axis_pairs)
+    return RopeDesc(batch, rows, n_q_heads, n_kv_heads, head_dim, rot_dim, layout, len(pairs), (ctypes.c_int32 * 3)(*pairs[:3]), float(magnitude), int(bool(backward)))
+
+
+def massv_rope_frequencies(rot_dim, base=10000.0, kind=ROPE_SCALE_NONE, factor=1.0, original_context=0.0, slow=1.0, fast=32.0, inv_freq=None,
+                           device="cuda") -> torch.Tensor:
+    """Turns per position as 64-bit fractions (int64 [rot_dim / 2] on ``device``), once per model."""
+    n = max(0, rot_dim // 2)
+    given = None
+    if inv_freq is not None:
+        given = (ctypes.c_double * len(inv_freq))(*[float(f) for f in inv_freq])
+        if len(inv_freq) != n:
+            raise ValueError(f"massv: inv_freq must have {n} values")
+    scaling = _RopeScaling(int(kind), float(factor), float(original_context), float(slow), float(fast), given)
+    turns = (ctypes.c_uint64 * max(1, n))()
+    rc = _lib.massv_rope_frequencies(rot_dim, float(base), ctypes.byref(scaling), turns)
+    if rc != 0:
+        raise MassvError(rc, "massv_rope_frequencies")
+    return torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device=device)
+
+
+def massv_rotary(desc, turns, q, k, q_out, k_out, positions=None, seq_lens=None, pos_delta=None) -> None:
+    """q, k and their outputs: bf16 [..., heads, head_dim] with evenly spaced tokens (slices of a fused projection's output are
+    fine); the outputs may be the inputs.  None for a side without heads."""
+    rc = _native.rotary(desc, turns, q, k, q_out, k_out, positions, seq_lens, pos_delta)
+    if rc != 0:
+        raise MassvError(rc, "massv_rotary")
+
+
+# ---- attention over a shared prefix
+def massv_verify_attn_shared_workspace_size(desc: AttnDesc, n_groups: int) -> int:
+    return int(_lib.massv_verify_attn_shared_workspace_size(ctypes.byref(desc), n_groups))
+
+
+def massv_verify_attn_shared(desc, group_start, shared_lens, q, k_new, v_new, k_pages, v_pages, page_table, seq_lens, out, out_f32=None, lse=None,
+                             workspace=None, dev_status=None) -> None:
+    """massv_verify_attn with the first ``shared_lens[g]`` positions of the sequences ``group_start[g] .. group_start[g + 1] - 1`` read once."""
+    rc = _native.verify_attn_shared(desc, group_start, shared_lens, q, k_new, v_new, k_pages, v_pages, page_table, seq_lens, out, out_f32, lse, workspace,
+                                    dev_status)
+    if rc != 0:
+        raise MassvError(rc, "massv_verify_attn_shared")
+
+
+# ---- rules on logits
+def logit_rules(allowed=None, bias_start=None, bias_tokens=None, bias_values=None, prompt_bits=None, output_bits=None, counts=None, repetition=None,
+                frequency=None, presence=None) -> LogitRules:
+    """Bit masks and indices int32, values fp32 (include/massv.h); the object keeps the tensors alive and is good for any number of calls."""
+    f32, i32 = torch.float32, torch.int32
+    r = LogitRules(_ptr(allowed, i32), _ptr(bias_start, i32), _ptr(bias_tokens, i32), _ptr(bias_values, f32), 0, _ptr(prompt_bits, i32), _ptr(output_bits, i32),
+                   _ptr(counts, i32), _ptr(repetition, f32), _ptr(frequency, f32), _ptr(presence, f32))
+    if bias_tokens is not None:
+        if bias_values is None or bias_values.numel() != bias_tokens.numel():
+            raise ValueError("massv: bias_tokens and bias_values must have the same length")
+        r.n_bias = bias_tokens.numel()
+    r.tensors = (allowed, bias_start, bias_tokens, bias_values, prompt_bits, output_bits, counts, repetition, frequency, presence)
+    return r
+
+
+def massv_logits_apply(gamma, rules, logits, logits_out, draft_tokens=None, dev_status=None) -> None:
+    """logits fp32 [batch, gamma + 1, V] (or [batch, V] with gamma 0); logits_out may be logits."""
+    vocab, rows = logits.shape[-1], gamma + 1
+    if logits.numel() != logits_out.numel() or logits.numel() % (rows * vocab or 1) != 0:
+        raise ValueError("massv: logits and logits_out must be [batch, gamma + 1, vocab]")
+    rc = _native.logits_apply(logits.numel() // (rows * vocab or 1), gamma, vocab, rules, logits, logits_out, draft_tokens, dev_status)
+    if rc != 0:
+        raise MassvError(rc, "massv_logits_apply")
+
+
+def massv_accept_logits_workspace_size(desc: AcceptDesc) -> int:
+    return int(_lib.massv_accept_logits_workspace_size(ctypes.byref(desc)))
+
+
+def massv_accept_logits(desc, rules, logits, logits_out, draft_tokens, draft_probs, u_accept, u_sample, out_tokens, accept_len, probs_out=None,
+                        workspace=None, dev_status=None) -> None:
+    """massv_accept from logits, under rules (None: none; logits_out may then be None too)."""
+    rc = _native.accept_logits(desc, rules, logits, logits_out, draft_tokens, draft_probs, u_accept, u_sample, out_tokens, accept_len, probs_out, workspace,
+                               dev_status)
+    if rc != 0:
+        raise MassvError(rc, "massv_accept_logits")
+
+
+def massv_history_add(vocab, tokens, lens, bits, counts=None, dev_status=None) -> None:
+    """Adds the first lens[b] of tokens[b] (int32 [batch, n]) to the bits (int32 [batch, ceil(vocab / 32)]) and counts (int32 [batch, vocab])."""
+    batch, n_max = tokens.shape
+    rc = _native.history_add(batch, vocab, tokens, n_max, lens, bits, counts, dev_status)
+    if rc != 0:
+        raise MassvError(rc, "massv_history_add")
 
 
 # ---- vocabulary shards (argument marshalling only; the caller moves the gathered buffers between ranks)

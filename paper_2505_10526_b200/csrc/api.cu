@@ -90,6 +90,80 @@ AttnLayout attn_layout(const massv_attn_desc& d) {
     return l;
 }
 
+// The call's parameters with its scratch (attn_layout) at ws.
+AttnParams attn_params(const massv_attn_desc* desc, const AttnLayout& l, const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                       const int32_t* page_table, const int32_t* seq_lens, void* out, float* out_f32, float* lse, char* ws, int32_t* dev_status) {
+    AttnParams p;
+    p.B = desc->batch; p.R = desc->gamma + 1; p.Hq = desc->n_q_heads; p.Hkv = desc->n_kv_heads;
+    p.d = desc->head_dim; p.max_pages = desc->max_pages_per_seq; p.num_pages = desc->num_pages;
+    p.scale = desc->scale > 0.f ? desc->scale : 1.f / sqrtf((float)desc->head_dim);
+    p.kv_chunk = l.kv_chunk; p.max_chunks = l.max_chunks; p.window = desc->window;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k_new = static_cast<const __nv_bfloat16*>(k_new);
+    p.v_new = static_cast<const __nv_bfloat16*>(v_new);
+    p.k_pages = static_cast<__nv_bfloat16*>(k_pages);
+    p.v_pages = static_cast<__nv_bfloat16*>(v_pages);
+    p.page_table = page_table; p.seq_lens = seq_lens;
+    p.out = static_cast<__nv_bfloat16*>(out); p.out_f32 = out_f32; p.lse = lse;
+    p.part_o = reinterpret_cast<float*>(ws + l.off_o);
+    p.part_ml = reinterpret_cast<float*>(ws + l.off_ml);
+    p.dev_status = dev_status;
+    p.path = (int)desc->flags;
+    p.chunk_forced = desc->kv_chunk > 0;
+    p.flat_part_o = reinterpret_cast<float*>(ws + l.off_flat_o);
+    p.flat_part_ml = reinterpret_cast<float*>(ws + l.off_flat_ml);
+    p.flat_meta = reinterpret_cast<int32_t*>(ws + l.off_flat_meta);
+    return p;
+}
+
+int check_attn_args(const void* q, const void* k_new, const void* v_new, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                    const int32_t* seq_lens, const void* out, const float* out_f32) {
+    if (!q || !k_new || !v_new || !k_pages || !v_pages || !page_table || !seq_lens || !out) return MASSV_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages) ||
+        !aligned16(out) || (out_f32 && !aligned16(out_f32)))
+        return MASSV_ERR_INVALID_ARG;
+    return MASSV_OK;
+}
+
+// What massv_verify_attn_shared needs: the attention call's own scratch (for what the sequences do not share), then the rest.
+struct SharedLayout {
+    AttnLayout attn;
+    int slot_tiles;
+    size_t off_groups, off_skip, off_lens, off_meta, off_table, off_out, off_lse, off_part_o, off_part_ml, total;
+};
+
+SharedLayout shared_layout(const massv_attn_desc& d, int n_groups) {
+    SharedLayout l;
+    l.attn = attn_layout(d);
+    const size_t B = d.batch, rows = B * (d.gamma + 1) * d.n_q_heads;
+    l.slot_tiles = shared_attn_slot_tiles(d.head_dim, (long)(rows / d.n_kv_heads));
+    size_t off = align_up(l.attn.total, kAlign);
+    auto take = [&](size_t bytes) { const size_t at = off; off += align_up(bytes, kAlign); return at; };
+    l.off_groups = take((size_t)n_groups * sizeof(int4));
+    l.off_skip = take(B * sizeof(int32_t));
+    l.off_lens = take(B * sizeof(int32_t));
+    l.off_meta = take((size_t)(n_groups + 2) * sizeof(int32_t));
+    l.off_table = take(B * d.max_pages_per_seq * sizeof(int32_t));
+    l.off_out = take(rows * d.head_dim * sizeof(float));
+    l.off_lse = take(rows * sizeof(float));
+    const size_t slots = (size_t)2 * kPrefixMaxCtas * l.slot_tiles * 128;
+    l.off_part_o = take(slots * d.head_dim * sizeof(float));
+    l.off_part_ml = take(slots * 2 * sizeof(float));
+    l.total = off;
+    return l;
+}
+
+int check_shared(const massv_attn_desc* d, int32_t n_groups) {
+    const int rc = check_attn_desc(d);
+    if (rc != MASSV_OK) return rc;
+    if (n_groups < 1) return MASSV_ERR_INVALID_ARG;
+    if (n_groups > kMaxGroups || d->window != 0) return MASSV_ERR_UNSUPPORTED;
+    // the prefix kernel counts (tile, KV head, block) products of all groups in 32 bits
+    const double pairs = 128 / (d->n_q_heads / d->n_kv_heads), tiles = (double)d->batch * (d->gamma + 1) / pairs + n_groups;
+    if (tiles * d->n_kv_heads * ((double)d->max_pages_per_seq * kPageSize / kPrefixBlock) > 1e9) return MASSV_ERR_UNSUPPORTED;
+    return MASSV_OK;
+}
+
 int check_accept_desc(const massv_accept_desc* d) {
     if (!d) return MASSV_ERR_INVALID_ARG;
     if (d->batch < 1 || d->gamma < 0 || d->hidden < 1 || d->vocab < 1 || !(d->temperature >= 0.f))
@@ -147,36 +221,49 @@ int massv_verify_attn(const massv_attn_desc* desc, const void* q, const void* k_
     NvtxRange range("massv_verify_attn");
     const int rc = check_attn_desc(desc);
     if (rc != MASSV_OK) return rc;
-    if (!q || !k_new || !v_new || !k_pages || !v_pages || !page_table || !seq_lens || !out) return MASSV_ERR_INVALID_ARG;
-    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages) ||
-        !aligned16(out) || (out_f32 && !aligned16(out_f32)))
-        return MASSV_ERR_INVALID_ARG;
+    const int args = check_attn_args(q, k_new, v_new, k_pages, v_pages, page_table, seq_lens, out, out_f32);
+    if (args != MASSV_OK) return args;
     const AttnLayout l = attn_layout(*desc);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0 || workspace_bytes < l.total)
         return MASSV_ERR_WORKSPACE;
 
-    AttnParams p;
-    p.B = desc->batch; p.R = desc->gamma + 1; p.Hq = desc->n_q_heads; p.Hkv = desc->n_kv_heads;
-    p.d = desc->head_dim; p.max_pages = desc->max_pages_per_seq; p.num_pages = desc->num_pages;
-    p.scale = desc->scale > 0.f ? desc->scale : 1.f / sqrtf((float)desc->head_dim);
-    p.kv_chunk = l.kv_chunk; p.max_chunks = l.max_chunks; p.window = desc->window;
-    p.q = static_cast<const __nv_bfloat16*>(q);
-    p.k_new = static_cast<const __nv_bfloat16*>(k_new);
-    p.v_new = static_cast<const __nv_bfloat16*>(v_new);
-    p.k_pages = static_cast<__nv_bfloat16*>(k_pages);
-    p.v_pages = static_cast<__nv_bfloat16*>(v_pages);
-    p.page_table = page_table; p.seq_lens = seq_lens;
-    p.out = static_cast<__nv_bfloat16*>(out); p.out_f32 = out_f32; p.lse = lse;
-    char* ws = static_cast<char*>(workspace);
-    p.part_o = reinterpret_cast<float*>(ws + l.off_o);
-    p.part_ml = reinterpret_cast<float*>(ws + l.off_ml);
-    p.dev_status = dev_status;
-    p.path = (int)desc->flags;
-    p.chunk_forced = desc->kv_chunk > 0;
-    p.flat_part_o = reinterpret_cast<float*>(ws + l.off_flat_o);
-    p.flat_part_ml = reinterpret_cast<float*>(ws + l.off_flat_ml);
-    p.flat_meta = reinterpret_cast<int32_t*>(ws + l.off_flat_meta);
+    const AttnParams p = attn_params(desc, l, q, k_new, v_new, k_pages, v_pages, page_table, seq_lens, out, out_f32, lse, static_cast<char*>(workspace), dev_status);
     return launch_verify_attn(p, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
+}
+
+size_t massv_verify_attn_shared_workspace_size(const massv_attn_desc* desc, int32_t n_groups) {
+    if (check_shared(desc, n_groups) != MASSV_OK) return 0;
+    return shared_layout(*desc, n_groups).total;
+}
+
+int massv_verify_attn_shared(const massv_attn_desc* desc, int32_t n_groups, const int32_t* group_start, const int32_t* shared_lens,
+                             const void* q, const void* k_new, const void* v_new, void* k_pages, void* v_pages, const int32_t* page_table,
+                             const int32_t* seq_lens, void* out, float* out_f32, float* lse, void* workspace, size_t workspace_bytes,
+                             int32_t* dev_status, massv_stream_t stream) {
+    NvtxRange range("massv_verify_attn_shared");
+    const int rc = check_shared(desc, n_groups);
+    if (rc != MASSV_OK) return rc;
+    const int args = check_attn_args(q, k_new, v_new, k_pages, v_pages, page_table, seq_lens, out, out_f32);
+    if (args != MASSV_OK || !group_start || !shared_lens) return MASSV_ERR_INVALID_ARG;
+    const SharedLayout l = shared_layout(*desc, n_groups);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0 || workspace_bytes < l.total) return MASSV_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(workspace);
+    SharedAttnParams p;
+    p.a = attn_params(desc, l.attn, q, k_new, v_new, k_pages, v_pages, page_table, seq_lens, out, out_f32, lse, ws, dev_status);
+    p.n_groups = n_groups; p.group_start = group_start; p.shared_lens = shared_lens;
+    p.groups = reinterpret_cast<int4*>(ws + l.off_groups);
+    p.skip = reinterpret_cast<int32_t*>(ws + l.off_skip);
+    p.tail_lens = reinterpret_cast<int32_t*>(ws + l.off_lens);
+    p.tail_table = reinterpret_cast<int32_t*>(ws + l.off_table);
+    // sequences that share nothing are finished by the kernels of the rest: they write the caller's buffers where there are any
+    p.tail_out = out_f32 ? out_f32 : reinterpret_cast<float*>(ws + l.off_out);
+    p.tail_lse = lse ? lse : reinterpret_cast<float*>(ws + l.off_lse);
+    p.meta = reinterpret_cast<int32_t*>(ws + l.off_meta);
+    p.slot_tiles = l.slot_tiles;
+    p.part_o = reinterpret_cast<float*>(ws + l.off_part_o);
+    p.part_ml = reinterpret_cast<float*>(ws + l.off_part_ml);
+    const AttnParams rest = attn_params(desc, l.attn, q, k_new, v_new, k_pages, v_pages, p.tail_table, p.tail_lens, out, p.tail_out, p.tail_lse, ws, dev_status);
+    return launch_shared_attn(p, rest, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
 }
 
 size_t massv_accept_workspace_size(const massv_accept_desc* desc) {
@@ -477,6 +564,216 @@ int massv_sample_top_p(int32_t rows, int32_t vocab, float temperature, float top
     t.rows = rows; t.V = vocab; t.inv_T = 1.f / temperature; t.top_p = top_p;
     t.logits = logits; t.u = u; t.tokens = tokens; t.probs_out = probs_out; t.dev_status = dev_status;
     return launch_top_p(t, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
+}
+
+int massv_rope_frequencies(int32_t rot_dim, double base, const massv_rope_scaling* scaling, uint64_t* turns) {
+    if (rot_dim < 2 || rot_dim % 2 != 0 || !turns) return MASSV_ERR_INVALID_ARG;
+    if (rot_dim > 256) return MASSV_ERR_UNSUPPORTED;
+    const int kind = scaling ? scaling->kind : MASSV_ROPE_SCALE_NONE;
+    if (kind < MASSV_ROPE_SCALE_NONE || kind > MASSV_ROPE_SCALE_GIVEN) return MASSV_ERR_UNSUPPORTED;
+    if (kind == MASSV_ROPE_SCALE_GIVEN ? !scaling->inv_freq : !(base > 1.0 && base < HUGE_VAL)) return MASSV_ERR_INVALID_ARG;
+    const bool by_parts = kind == MASSV_ROPE_SCALE_TURNS || kind == MASSV_ROPE_SCALE_PAIRS;
+    if (kind != MASSV_ROPE_SCALE_NONE && kind != MASSV_ROPE_SCALE_GIVEN && !(scaling->factor >= 1.0 && scaling->factor < HUGE_VAL)) return MASSV_ERR_INVALID_ARG;
+    if (by_parts && !(scaling->original_context > 0.0 && scaling->original_context < HUGE_VAL && scaling->slow > 0.0 && scaling->fast > scaling->slow && scaling->fast < HUGE_VAL))
+        return MASSV_ERR_INVALID_ARG;
+    if (kind == MASSV_ROPE_SCALE_BASE && rot_dim == 2) return MASSV_ERR_UNSUPPORTED;
+    const long double two_pi = 6.283185307179586476925286766559005768L;
+    long double b = base;
+    if (kind == MASSV_ROPE_SCALE_BASE) b *= powl(scaling->factor, (long double)rot_dim / (rot_dim - 2));
+    long double lo = 0, hi = 0;
+    if (kind == MASSV_ROPE_SCALE_PAIRS) {
+        const auto index = [&](long double t) { return rot_dim * logl(scaling->original_context / (two_pi * t)) / (2 * logl(b)); };
+        const auto clamped = [&](long double x) { return x < 0 ? 0.0L : x > rot_dim - 1 ? (long double)(rot_dim - 1) : x; };
+        lo = clamped(floorl(index(scaling->fast)));
+        hi = clamped(ceill(index(scaling->slow)));
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        long double f = kind == MASSV_ROPE_SCALE_GIVEN ? (long double)scaling->inv_freq[i] : powl(b, -2.0L * i / rot_dim);
+        if (!isfinite((double)f)) return MASSV_ERR_INVALID_ARG;
+        if (kind == MASSV_ROPE_SCALE_LINEAR) f /= scaling->factor;
+        if (by_parts) {
+            long double w;
+            if (kind == MASSV_ROPE_SCALE_TURNS) w = (scaling->original_context * f / two_pi - scaling->slow) / (scaling->fast - scaling->slow);
+            else w = hi > lo ? 1 - (i - lo) / (hi - lo) : i <= lo ? 1.0L : 0.0L;
+            w = w < 0 ? 0 : w > 1 ? 1 : w;
+            f *= w + (1 - w) / scaling->factor;
+        }
+        long double t = f / two_pi;
+        t -= floorl(t);                                        // whole turns do not show
+        const long double scaled = roundl(t * 18446744073709551616.0L);
+        turns[i] = scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
+    }
+    return MASSV_OK;
+}
+
+int massv_rotary(const massv_rope_desc* desc, const uint64_t* turns, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                 const int32_t* positions, const int32_t* seq_lens, const int32_t* pos_delta, void* q_out, int64_t q_out_stride, void* k_out,
+                 int64_t k_out_stride, massv_stream_t stream) {
+    NvtxRange range("massv_rotary");
+    if (!desc || !turns) return MASSV_ERR_INVALID_ARG;
+    const massv_rope_desc& d = *desc;
+    if (d.batch < 1 || d.rows < 1 || d.n_q_heads < 0 || d.n_kv_heads < 0 || d.n_q_heads + (int64_t)d.n_kv_heads < 1 || !isfinite(d.magnitude)) return MASSV_ERR_INVALID_ARG;
+    if ((int64_t)d.batch * d.rows > 0x7fffffff || d.head_dim < 8 || d.head_dim > 256 || d.head_dim % 8 != 0 || d.rot_dim < 2 || d.rot_dim % 2 != 0 ||
+        d.rot_dim > d.head_dim || (d.layout != MASSV_ROPE_HALF && d.layout != MASSV_ROPE_INTERLEAVED) || d.n_axes < 1 || d.n_axes > 3 ||
+        d.flags > MASSV_ROPE_BACKWARD || d.n_q_heads + (int64_t)d.n_kv_heads > 65536)
+        return MASSV_ERR_UNSUPPORTED;
+    int64_t sum = 0;
+    for (int a = 0; a < d.n_axes; ++a) {
+        if (d.axis_pairs[a] < 0) return MASSV_ERR_INVALID_ARG;
+        sum += d.axis_pairs[a];
+    }
+    if (sum != d.rot_dim / 2) return MASSV_ERR_INVALID_ARG;
+    if (!positions == !seq_lens || (positions && pos_delta)) return MASSV_ERR_INVALID_ARG;
+    const auto bad = [&](const void* p, int64_t stride, int heads) {
+        return heads > 0 && (!p || !aligned16(p) || stride % 8 != 0 || stride < (int64_t)heads * d.head_dim);
+    };
+    if (bad(q, q_stride, d.n_q_heads) || bad(q_out, q_out_stride, d.n_q_heads) || bad(k, k_stride, d.n_kv_heads) || bad(k_out, k_out_stride, d.n_kv_heads) ||
+        reinterpret_cast<uintptr_t>(turns) % 8 != 0)
+        return MASSV_ERR_INVALID_ARG;
+    const bool q_same = d.n_q_heads == 0 || q == q_out, k_same = d.n_kv_heads == 0 || k == k_out;
+    if ((d.n_q_heads > 0 && q == q_out && q_stride != q_out_stride) || (d.n_kv_heads > 0 && k == k_out && k_stride != k_out_stride)) return MASSV_ERR_INVALID_ARG;
+    RopeParams p{};
+    p.B = d.batch; p.rows = d.rows; p.Hq = d.n_q_heads; p.Hkv = d.n_kv_heads; p.d = d.head_dim; p.rot_dim = d.rot_dim; p.n_axes = d.n_axes;
+    p.axis_end[0] = d.n_axes > 1 ? d.axis_pairs[0] : d.rot_dim / 2;
+    p.axis_end[1] = d.n_axes > 2 ? d.axis_pairs[0] + d.axis_pairs[1] : d.rot_dim / 2;
+    p.half = d.layout == MASSV_ROPE_HALF; p.backward = d.flags != 0; p.copy = !(q_same && k_same) && d.rot_dim < d.head_dim;
+    p.magnitude = d.magnitude; p.turns = turns;
+    p.q = static_cast<const __nv_bfloat16*>(q); p.k = static_cast<const __nv_bfloat16*>(k);
+    p.q_out = static_cast<__nv_bfloat16*>(q_out); p.k_out = static_cast<__nv_bfloat16*>(k_out);
+    p.q_stride = q_stride; p.k_stride = k_stride; p.q_out_stride = q_out_stride; p.k_out_stride = k_out_stride;
+    p.positions = positions; p.seq_lens = seq_lens; p.pos_delta = pos_delta;
+    return launch_rope(p, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
+}
+
+}  // extern "C"
+
+namespace {
+int check_rules(const massv_logit_rules* r) {
+    if (!r) return MASSV_ERR_INVALID_ARG;
+    if (r->bias_start ? (r->n_bias < 0 || (r->n_bias > 0 && (!r->bias_tokens || !r->bias_values))) : false) return MASSV_ERR_INVALID_ARG;
+    if (!r->output_bits != !r->counts) return MASSV_ERR_INVALID_ARG;
+    return MASSV_OK;
+}
+// Only what some rule reads is looked at: the prompt matters to the repetition penalty alone, the output and the drafts to any of the three.
+void set_rules(LogitsParams& p, const massv_logit_rules* r, const int32_t* drafts) {
+    p.allowed = r->allowed;
+    p.bias_start = r->n_bias > 0 ? r->bias_start : nullptr; p.bias_tokens = r->bias_tokens; p.bias_values = r->bias_values; p.n_bias = r->n_bias;
+    p.repetition = r->repetition; p.frequency = r->frequency; p.presence = r->presence;
+    const bool any = r->repetition || r->frequency || r->presence;
+    p.prompt_bits = r->repetition ? r->prompt_bits : nullptr;
+    p.output_bits = any ? r->output_bits : nullptr; p.counts = any ? r->counts : nullptr;
+    p.drafts = any && p.R > 1 ? drafts : nullptr;
+}
+
+struct AcceptLogitsLayout {
+    int n_part, n_chunks;
+    size_t off_max, off_sum, off_idx, off_state, off_chunks, off_segs, off_counters, off_rowstat, total;
+};
+AcceptLogitsLayout accept_logits_layout(const massv_accept_desc& d) {
+    AcceptLogitsLayout l;
+    const size_t M = (size_t)d.batch * (d.gamma + 1);
+    l.n_part = logit_slices(d.vocab);
+    l.n_chunks = (d.vocab + kResidualChunk - 1) / kResidualChunk;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off += align_up(bytes, kAlign); return at; };
+    l.off_max = take((size_t)l.n_part * M * sizeof(float));
+    l.off_sum = take((size_t)l.n_part * M * sizeof(float));
+    l.off_idx = take((size_t)l.n_part * M * sizeof(int32_t));
+    l.off_state = take((size_t)d.batch * sizeof(SeqState));
+    l.off_chunks = take((size_t)d.batch * l.n_chunks * sizeof(double));
+    l.off_segs = take(d.temperature > 0.f ? (size_t)d.batch * l.n_chunks * kResidualSegments * sizeof(double) : 0);
+    l.off_counters = take((size_t)d.batch * sizeof(unsigned int));
+    l.off_rowstat = take(M * 2 * sizeof(float));
+    l.total = off;
+    return l;
+}
+// The acceptance call's limits; `hidden` does not matter here.
+int check_accept_logits_desc(const massv_accept_desc* desc) {
+    if (!desc) return MASSV_ERR_INVALID_ARG;
+    massv_accept_desc d = *desc;
+    d.hidden = 64;
+    return check_accept_desc(&d);
+}
+}  // namespace
+
+extern "C" {
+
+int massv_logits_apply(int32_t batch, int32_t gamma, int32_t vocab, const massv_logit_rules* rules, const float* logits, float* logits_out,
+                       const int32_t* draft_tokens, int32_t* dev_status, massv_stream_t stream) {
+    NvtxRange range("massv_logits_apply");
+    if (batch < 1 || gamma < 0 || vocab < 1 || !logits || !logits_out) return MASSV_ERR_INVALID_ARG;
+    if (batch > 65535 || gamma > kMaxRows - 1 || vocab > (1 << 21)) return MASSV_ERR_UNSUPPORTED;
+    const int rc = check_rules(rules);
+    if (rc != MASSV_OK) return rc;
+    if (!aligned16(logits) || !aligned16(logits_out)) return MASSV_ERR_INVALID_ARG;
+    LogitsParams p{};
+    p.B = batch; p.R = gamma + 1; p.V = vocab; p.logits = logits; p.out = logits_out; p.dev_status = dev_status;
+    set_rules(p, rules, draft_tokens);
+    return launch_logit_rules(p, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
+}
+
+size_t massv_accept_logits_workspace_size(const massv_accept_desc* desc) {
+    if (check_accept_logits_desc(desc) != MASSV_OK) return 0;
+    return accept_logits_layout(*desc).total;
+}
+
+int massv_accept_logits(const massv_accept_desc* desc, const massv_logit_rules* rules, const float* logits, float* logits_out,
+                        const int32_t* draft_tokens, const float* draft_probs, const float* u_accept, const float* u_sample, int32_t* out_tokens,
+                        int32_t* accept_len, float* probs_out, void* workspace, size_t workspace_bytes, int32_t* dev_status, massv_stream_t stream) {
+    NvtxRange range("massv_accept_logits");
+    int rc = check_accept_logits_desc(desc);
+    if (rc != MASSV_OK) return rc;
+    if (desc->flags != 0) return MASSV_ERR_UNSUPPORTED;
+    const bool sampling = desc->temperature > 0.f;
+    if (!logits || !out_tokens || !accept_len || (desc->gamma > 0 && !draft_tokens)) return MASSV_ERR_INVALID_ARG;
+    if (sampling && (!u_sample || (desc->gamma > 0 && (!draft_probs || !u_accept)))) return MASSV_ERR_INVALID_ARG;
+    if (!sampling && probs_out) return MASSV_ERR_INVALID_ARG;
+    if (rules) {
+        rc = check_rules(rules);
+        if (rc != MASSV_OK) return rc;
+        if (sampling && !logits_out) return MASSV_ERR_INVALID_ARG;
+    }
+    if (!aligned16(logits) || (logits_out && !aligned16(logits_out)) || (draft_probs && !aligned16(draft_probs)) || (probs_out && !aligned16(probs_out)))
+        return MASSV_ERR_INVALID_ARG;
+    const AcceptLogitsLayout l = accept_logits_layout(*desc);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0 || workspace_bytes < l.total) return MASSV_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(workspace);
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    LogitsParams p{};
+    p.B = desc->batch; p.R = desc->gamma + 1; p.V = desc->vocab; p.logits = logits; p.dev_status = dev_status;
+    if (rules) {
+        p.out = logits_out;
+        set_rules(p, rules, draft_tokens);
+    }
+    p.greedy = sampling ? 0 : 1;
+    p.inv_T_log2e = sampling ? 1.4426950408889634f / desc->temperature : 0.f;
+    p.part_max = reinterpret_cast<float*>(ws + l.off_max);
+    p.part_sum = reinterpret_cast<float*>(ws + l.off_sum);
+    p.part_idx = reinterpret_cast<int32_t*>(ws + l.off_idx);
+    if (launch_logit_rules(p, s) != cudaSuccess) return MASSV_ERR_CUDA;
+
+    AcceptParams a{};
+    a.B = desc->batch; a.gamma = desc->gamma; a.V = desc->vocab; a.T = desc->temperature;
+    a.n_part = l.n_part; a.part_max = p.part_max; a.part_sum = p.part_sum; a.part_idx = p.part_idx;
+    a.logits = rules ? logits_out : logits;
+    a.draft_tokens = draft_tokens; a.draft_probs = draft_probs; a.u_accept = u_accept; a.u_sample = u_sample;
+    a.out_tokens = out_tokens; a.accept_len = accept_len; a.probs_out = probs_out;
+    a.seq_state = reinterpret_cast<SeqState*>(ws + l.off_state);
+    a.chunk_sums = reinterpret_cast<double*>(ws + l.off_chunks);
+    a.seg_sums = sampling ? reinterpret_cast<double*>(ws + l.off_segs) : nullptr;
+    a.counters = reinterpret_cast<unsigned int*>(ws + l.off_counters);
+    a.row_stats = reinterpret_cast<float*>(ws + l.off_rowstat);
+    a.n_chunks = l.n_chunks;
+    a.dev_status = dev_status;
+    return launch_accept(a, s) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
+}
+
+int massv_history_add(int32_t batch, int32_t vocab, const int32_t* tokens, int32_t n_max, const int32_t* lens, uint32_t* bits, int32_t* counts,
+                      int32_t* dev_status, massv_stream_t stream) {
+    if (batch < 1 || vocab < 1 || n_max < 0 || !bits || (n_max > 0 && !tokens)) return MASSV_ERR_INVALID_ARG;
+    if ((int64_t)batch * n_max > ((int64_t)1 << 38)) return MASSV_ERR_UNSUPPORTED;
+    return launch_history_add(batch, vocab, tokens, n_max, lens, bits, counts, dev_status, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? MASSV_OK
+                                                                                                                                              : MASSV_ERR_CUDA;
 }
 
 int massv_kv_commit(int32_t batch, int32_t gamma, const int32_t* accept_len, int32_t* seq_lens, int32_t* dev_status,

@@ -48,6 +48,26 @@ bool attn_use_umma(const AttnParams& p);
 cudaError_t launch_attn_umma(const AttnParams& p, const CUtensorMap& map_k, const CUtensorMap& map_v, cudaStream_t stream, bool flat,
                              int* launched, cudaEvent_t split_done);
 
+// ---------------------------------------------------------------- attention over a shared prefix
+constexpr int kPrefixBlock = 128;      // positions of a block of the prefix
+constexpr int kMaxGroups = 256;
+constexpr int kPrefixMaxCtas = 160;    // resident CTAs of the prefix kernel, one per SM
+struct SharedAttnParams {
+    AttnParams a;                      // the call as it stands: queries, pools, the caller's page tables and lengths, outputs
+    int n_groups;
+    const int32_t *group_start, *shared_lens;
+    int4* groups;                      // [n_groups] blocks of the shared prefix, the sequence whose table is read, first (sequence, row) pair, pairs
+    int32_t* skip;                     // [B] positions that the prefix kernel covers
+    int32_t *tail_lens, *tail_table;   // [B], [B, max_pages]: lengths and tables behind them
+    float *tail_out, *tail_lse;        // [B, R, Hq, d], [B, R, Hq]: the rest's result (the caller's out_f32 and lse where they are given)
+    int32_t* meta;                     // [0] units per CTA, [1 + g] units of groups 0 .. g-1
+    int slot_tiles;                    // tiles a slot has room for
+    float *part_o, *part_ml;           // [2 * kPrefixMaxCtas, slot_tiles, 128, d], [.., 128, 2]: pieces
+};
+int shared_attn_slot_tiles(int d, long rows);      // rows: query rows of all sequences per KV head
+// rest: the same call on tail_table, tail_lens, tail_out and tail_lse
+cudaError_t launch_shared_attn(const SharedAttnParams& p, const AttnParams& rest, cudaStream_t stream);
+
 // ---------------------------------------------------------------- LM head
 struct LmHeadParams {
     int M, K, V;
@@ -162,6 +182,46 @@ struct TopPParams {
     int32_t* dev_status;
 };
 cudaError_t launch_top_p(const TopPParams& p, cudaStream_t stream);
+
+// ---------------------------------------------------------------- rotary positions
+struct RopeParams {
+    int B, rows, Hq, Hkv, d, rot_dim, n_axes;
+    int axis_end[2];                // pairs below axis_end[0] follow axis 0, below axis_end[1] axis 1, the others axis 2
+    bool half, backward;
+    bool copy;                      // elements behind rot_dim go to another place
+    float magnitude;
+    const uint64_t* turns;          // [rot_dim / 2]
+    const __nv_bfloat16 *q, *k;
+    __nv_bfloat16 *q_out, *k_out;
+    long long q_stride, k_stride, q_out_stride, k_out_stride;
+    const int32_t *positions, *seq_lens, *pos_delta;
+    int tokens_per_cta;             // set by the launch
+};
+cudaError_t launch_rope(const RopeParams& p, cudaStream_t stream);
+
+// ---------------------------------------------------------------- rules on logits
+constexpr int kLogitSlice = 1024;   // logits of one row that a warp takes; one partial slot of the row's statistics
+int logit_slices(int V);
+struct LogitsParams {
+    int B, R, V;
+    const float* logits;            // [B, R, V]
+    float* out;                     // [B, R, V] or nullptr; may be logits
+    const int32_t* drafts;          // [B, R - 1] or nullptr
+    // the rules (massv_logit_rules); nullptr: off
+    const uint32_t *allowed, *prompt_bits, *output_bits;
+    const int32_t *bias_start, *bias_tokens, *counts;
+    const float *bias_values, *repetition, *frequency, *presence;
+    int n_bias;
+    // statistics of the result, [logit_slices(V), B * R] each; part_max nullptr: none
+    int greedy;
+    float inv_T_log2e;
+    float *part_max, *part_sum;
+    int32_t* part_idx;
+    int32_t* dev_status;
+};
+cudaError_t launch_logit_rules(const LogitsParams& p, cudaStream_t stream);
+cudaError_t launch_history_add(int B, int V, const int32_t* tokens, int n_max, const int32_t* lens, uint32_t* bits, int32_t* counts,
+                               int32_t* dev_status, cudaStream_t stream);
 
 cudaError_t launch_kv_commit(int B, int gamma, const int32_t* accept_len, int32_t* seq_lens, int32_t* dev_status,
                              cudaStream_t stream);

@@ -6,6 +6,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <memory>
+
 #include "massv.h"
 
 namespace {
@@ -15,7 +17,12 @@ decltype(&massv_accept) g_accept = nullptr;
 decltype(&massv_kv_commit) g_kv_commit = nullptr;
 decltype(&massv_sample_top_p) g_sample_top_p = nullptr;
 decltype(&massv_tvd) g_tvd = nullptr;
-PyObject *g_attn_desc = nullptr, *g_accept_desc = nullptr;       // the ctypes structures of the two descriptors
+decltype(&massv_rotary) g_rotary = nullptr;
+decltype(&massv_verify_attn_shared) g_verify_attn_shared = nullptr;
+decltype(&massv_logits_apply) g_logits_apply = nullptr;
+decltype(&massv_accept_logits) g_accept_logits = nullptr;
+decltype(&massv_history_add) g_history_add = nullptr;
+PyObject *g_attn_desc = nullptr, *g_accept_desc = nullptr, *g_rope_desc = nullptr, *g_logit_rules = nullptr;       // the ctypes structures of the descriptors
 
 const char* dtype_name(c10::ScalarType t) {
     switch (t) {
@@ -48,6 +55,44 @@ float* f32(PyObject* o) { return static_cast<float*>(pointer(o, c10::ScalarType:
 int32_t* i32(PyObject* o) { return static_cast<int32_t*>(pointer(o, c10::ScalarType::Int)); }
 void* any(PyObject* o) { return pointer(o, c10::ScalarType::Undefined); }
 size_t elements(PyObject* o) { return o == Py_None ? 0 : (size_t)THPVariable_Unpack(o).numel(); }      // (behind any(): a tensor)
+
+// The same for a tensor that has to live on the device whose stream the call goes to.
+const at::Tensor& on_device(PyObject* obj) {
+    if (!THPVariable_Check(obj)) fail(PyExc_AttributeError, "massv: tensors expected");
+    const at::Tensor& t = THPVariable_Unpack(obj);
+    if (!t.is_cuda()) fail(PyExc_ValueError, "massv: tensors must live on a CUDA device");
+    if (t.get_device() != c10::cuda::current_device()) fail(PyExc_ValueError, "massv: tensors must live on the current device");
+    return t;
+}
+void* here(PyObject* obj, c10::ScalarType dtype) {
+    if (obj != Py_None) on_device(obj);
+    return pointer(obj, dtype);
+}
+
+// Tokens of heads * d consecutive bf16 elements, evenly spaced: a dense tensor [..., heads, d] or a slice of a fused projection's output.
+struct Tokens { void* data = nullptr; int64_t stride = 0; };
+Tokens tokens_of(PyObject* obj, int64_t n, int64_t heads, int64_t d) {
+    Tokens r;
+    if (obj == Py_None) return r;
+    const at::Tensor& t = on_device(obj);
+    if (t.scalar_type() != c10::ScalarType::BFloat16) {
+        PyErr_Format(PyExc_ValueError, "massv: expected torch.bfloat16, got %s", dtype_name(t.scalar_type()));
+        throw PythonError();
+    }
+    const int64_t dims = t.dim();
+    if (dims < 3 || t.size(dims - 1) != d || t.size(dims - 2) != heads || t.numel() != n * heads * d) fail(PyExc_ValueError, "massv: tokens must be [..., heads, head_dim], as many as the descriptor says");
+    if (t.stride(dims - 1) != 1 || (heads > 1 && t.stride(dims - 2) != d)) fail(PyExc_ValueError, "massv: a token's heads must be contiguous");
+    int64_t count = 1;
+    r.stride = heads * d;
+    for (int64_t i = dims - 3; i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        if (count == 1) r.stride = t.stride(i);
+        else if (t.stride(i) != r.stride * count) fail(PyExc_ValueError, "massv: tokens must be evenly spaced");
+        count *= t.size(i);
+    }
+    r.data = t.mutable_data_ptr();
+    return r;
+}
 
 // A descriptor: the bytes of its ctypes structure (or of one derived from it, which begins with the same fields).
 template <typename Desc>
@@ -160,14 +205,91 @@ PyObject* py_tvd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 9, [&] {
+        const DescOf<massv_rope_desc> d(a[0], g_rope_desc);
+        const massv_rope_desc& g = *d.get();
+        const int64_t count = (int64_t)g.batch * g.rows;
+        const uint64_t* turns = static_cast<const uint64_t*>(here(a[1], c10::ScalarType::Long));
+        const Tokens q = tokens_of(a[2], count, g.n_q_heads, g.head_dim), k = tokens_of(a[3], count, g.n_kv_heads, g.head_dim);
+        const Tokens qo = tokens_of(a[4], count, g.n_q_heads, g.head_dim), ko = tokens_of(a[5], count, g.n_kv_heads, g.head_dim);
+        int32_t *pos[3];
+        for (int i = 0; i < 3; ++i) pos[i] = static_cast<int32_t*>(here(a[6 + i], c10::ScalarType::Int));
+        const massv_stream_t s = stream();
+        return unlocked([&] { return g_rotary(d.get(), turns, q.data, q.stride, k.data, k.stride, pos[0], pos[1], pos[2], qo.data, qo.stride, ko.data, ko.stride, s); });
+    });
+}
+PyObject* py_verify_attn_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 15, [&] {
+        const DescOf<massv_attn_desc> d(a[0], g_attn_desc);
+        const auto in = [&](int i, c10::ScalarType t) { return here(a[i], t); };
+        constexpr auto BF = c10::ScalarType::BFloat16, I = c10::ScalarType::Int, F = c10::ScalarType::Float;
+        if (a[1] == Py_None || a[2] == Py_None) fail(PyExc_ValueError, "massv: groups expected");
+        int32_t *start = static_cast<int32_t*>(in(1, I)), *shared = static_cast<int32_t*>(in(2, I));
+        const int64_t groups = THPVariable_Unpack(a[2]).numel();
+        if (THPVariable_Unpack(a[1]).numel() != groups + 1) fail(PyExc_ValueError, "massv: group_start has one entry more than shared_lens");
+        void *q = in(3, BF), *kn = in(4, BF), *vn = in(5, BF), *kp = in(6, BF), *vp = in(7, BF);
+        int32_t *table = static_cast<int32_t*>(in(8, I)), *lens = static_cast<int32_t*>(in(9, I));
+        void* out = in(10, BF);
+        float *out32 = static_cast<float*>(in(11, F)), *lse = static_cast<float*>(in(12, F));
+        void* ws = in(13, c10::ScalarType::Undefined);
+        const size_t ws_bytes = elements(a[13]);
+        int32_t* status = static_cast<int32_t*>(in(14, I));
+        const massv_stream_t s = stream();
+        return unlocked([&] { return g_verify_attn_shared(d.get(), (int32_t)groups, start, shared, q, kn, vn, kp, vp, table, lens, out, out32, lse, ws, ws_bytes, status, s); });
+    });
+}
+PyObject* py_logits_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&] {
+        const int32_t batch = (int32_t)integer(a[0]), gamma = (int32_t)integer(a[1]), vocab = (int32_t)integer(a[2]);
+        const DescOf<massv_logit_rules> rules(a[3], g_logit_rules);
+        float *z = static_cast<float*>(here(a[4], c10::ScalarType::Float)), *out = static_cast<float*>(here(a[5], c10::ScalarType::Float));
+        int32_t *drafts = static_cast<int32_t*>(here(a[6], c10::ScalarType::Int)), *status = static_cast<int32_t*>(here(a[7], c10::ScalarType::Int));
+        const massv_stream_t s = stream();
+        return unlocked([&] { return g_logits_apply(batch, gamma, vocab, rules.get(), z, out, drafts, status, s); });
+    });
+}
+PyObject* py_accept_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&] {
+        const DescOf<massv_accept_desc> d(a[0], g_accept_desc);
+        const std::unique_ptr<DescOf<massv_logit_rules>> rules(a[1] == Py_None ? nullptr : new DescOf<massv_logit_rules>(a[1], g_logit_rules));
+        const auto f = [&](int i) { return static_cast<float*>(here(a[i], c10::ScalarType::Float)); };
+        const auto w = [&](int i) { return static_cast<int32_t*>(here(a[i], c10::ScalarType::Int)); };
+        float *z = f(2), *out = f(3);
+        int32_t* drafts = w(4);
+        float *q = f(5), *ua = f(6), *us = f(7);
+        int32_t *tokens = w(8), *lens = w(9);
+        float* probs = f(10);
+        void* ws = here(a[11], c10::ScalarType::Undefined);
+        const size_t ws_bytes = elements(a[11]);
+        int32_t* status = w(12);
+        const massv_stream_t s = stream();
+        return unlocked([&] { return g_accept_logits(d.get(), rules ? rules->get() : nullptr, z, out, drafts, q, ua, us, tokens, lens, probs, ws, ws_bytes, status, s); });
+    });
+}
+PyObject* py_history_add(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&] {
+        const int32_t batch = (int32_t)integer(a[0]), vocab = (int32_t)integer(a[1]), n_max = (int32_t)integer(a[3]);
+        const auto w = [&](int i) { return static_cast<int32_t*>(here(a[i], c10::ScalarType::Int)); };
+        int32_t *tokens = w(2), *lens = w(4), *bits = w(5), *counts = w(6), *status = w(7);
+        const massv_stream_t s = stream();
+        return unlocked([&] { return g_history_add(batch, vocab, tokens, n_max, lens, reinterpret_cast<uint32_t*>(bits), counts, status, s); });
+    });
+}
+
 PyObject* py_bind(PyObject*, PyObject* args) {
-    unsigned long long attn, accept, commit, top_p, tvd;
-    PyObject *attn_desc, *accept_desc;
-    if (!PyArg_ParseTuple(args, "KKKKKO!O!", &attn, &accept, &commit, &top_p, &tvd, &PyType_Type, &attn_desc, &PyType_Type, &accept_desc)) return nullptr;
-    Py_INCREF(attn_desc);
-    Py_INCREF(accept_desc);
-    Py_XSETREF(g_attn_desc, attn_desc);
-    Py_XSETREF(g_accept_desc, accept_desc);
+    unsigned long long attn, accept, commit, top_p, tvd, rotary, shared, apply, accept_logits, history;
+    PyObject *attn_desc, *accept_desc, *rope_desc, *logit_rules;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKO!O!O!O!", &attn, &accept, &commit, &top_p, &tvd, &rotary, &shared, &apply, &accept_logits, &history, &PyType_Type, &attn_desc,
+                          &PyType_Type, &accept_desc, &PyType_Type, &rope_desc, &PyType_Type, &logit_rules))
+        return nullptr;
+    const auto keep = [](PyObject*& slot, PyObject* type) { Py_INCREF(type); Py_XSETREF(slot, type); };
+    keep(g_attn_desc, attn_desc); keep(g_accept_desc, accept_desc); keep(g_rope_desc, rope_desc); keep(g_logit_rules, logit_rules);
+    g_rotary = reinterpret_cast<decltype(g_rotary)>(rotary);
+    g_verify_attn_shared = reinterpret_cast<decltype(g_verify_attn_shared)>(shared);
+    g_logits_apply = reinterpret_cast<decltype(g_logits_apply)>(apply);
+    g_accept_logits = reinterpret_cast<decltype(g_accept_logits)>(accept_logits);
+    g_history_add = reinterpret_cast<decltype(g_history_add)>(history);
     g_verify_attn = reinterpret_cast<decltype(g_verify_attn)>(attn);
     g_accept = reinterpret_cast<decltype(g_accept)>(accept);
     g_kv_commit = reinterpret_cast<decltype(g_kv_commit)>(commit);
@@ -184,6 +306,11 @@ PyMethodDef g_methods[] = {
     {"kv_commit", MASSV_FAST(py_kv_commit), nullptr},
     {"sample_top_p", MASSV_FAST(py_sample_top_p), nullptr},
     {"tvd", MASSV_FAST(py_tvd), nullptr},
+    {"rotary", MASSV_FAST(py_rotary), nullptr},
+    {"verify_attn_shared", MASSV_FAST(py_verify_attn_shared), nullptr},
+    {"logits_apply", MASSV_FAST(py_logits_apply), nullptr},
+    {"accept_logits", MASSV_FAST(py_accept_logits), nullptr},
+    {"history_add", MASSV_FAST(py_history_add), nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

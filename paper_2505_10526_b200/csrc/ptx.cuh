@@ -59,6 +59,14 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, i
         : "memory");
 }
 
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(smem_u32(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
+
 // Plain 1-D copies into shared memory, without an eviction hint: by the bulk engine (16-byte multiples, signalled on an mbarrier)
 // and by the calling thread.
 __device__ __forceinline__ void bulk_load_1d(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -98,5 +106,7 @@ bool make_tensor_map_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, 
 // The same matrix as a 3-D map [cols / 64, rows, 64], box [blocks, box_rows, 64]: one copy brings several groups of 64
 // columns (cols a multiple of 64; groups past the end are filled with zeros).
 bool make_tensor_map_bf16_blocks(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint32_t blocks);
+// [rows, heads, d] with boxes of box_heads heads of box_rows consecutive rows (64 elements of d); rows past the end come as zeros.
+bool make_tensor_map_bf16_heads(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint64_t d, uint32_t box_rows, uint32_t box_heads);
 
 }  // namespace massv

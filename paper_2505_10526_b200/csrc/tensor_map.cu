@@ -48,4 +48,17 @@ bool make_tensor_map_bf16_blocks(CUtensorMap* map, const void* base, uint64_t ro
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same over [rows, heads, d] with a box of [box_rows, box_heads, 64]: the box_heads heads of box_rows rows, one after the other.
+bool make_tensor_map_bf16_heads(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint64_t d, uint32_t box_rows, uint32_t box_heads) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {d, heads, rows};
+    const cuuint64_t strides[2] = {d * 2, heads * d * 2};
+    const cuuint32_t box[3] = {64, box_heads, box_rows};
+    const cuuint32_t elem[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, elem,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace massv

@@ -143,14 +143,14 @@ size_t massv_verify_attn_shared_workspace_size(const massv_attn_desc *desc, int3
  * samples of one prompt.  The result is that of massv_verify_attn on the same arguments (append included); the shared positions
  * are read and multiplied once per group instead of once per sequence.
  *
- *   n_groups        1 .. 256
+ *   desc->batch     at most 2048;  n_groups 1 .. 256
  *   group_start     int32 [n_groups + 1], 0 = group_start[0] <= ... <= group_start[n_groups] = B: group g is the sequences
  *                   group_start[g] .. group_start[g + 1] - 1.  Anything else stores MASSV_ERR_INVALID_ARG in dev_status, and nothing is shared.
  *   shared_lens     int32 [n_groups]: the first shared_lens[g] positions are the same for all sequences of group g, i.e. their
  *                   page tables have the same page ids for every page that lies wholly inside them.  More than a
  *                   member has committed is taken as the least of the members' lengths.  The ids are read from the group's first sequence.
  *   other arguments as for massv_verify_attn; desc->window must be 0 (MASSV_ERR_UNSUPPORTED otherwise: a local layer reads only
- *                   its window, with massv_verify_attn on the same page tables)
+ *                   its window, with massv_verify_attn on the same page tables); desc->kv_chunk and the kernel choice are not used
  * A group of one sequence, and what a group shares beyond whole blocks of 128 positions, are read per sequence.  A
  * sequence whose lengths violate the capacity rule is skipped, as in massv_verify_attn, and does not count as a member.
  */

@@ -125,30 +125,21 @@ int check_attn_args(const void* q, const void* k_new, const void* v_new, const v
     return MASSV_OK;
 }
 
-// What massv_verify_attn_shared needs: the attention call's own scratch (for what the sequences do not share), then the rest.
 struct SharedLayout {
-    AttnLayout attn;
-    int slot_tiles;
-    size_t off_groups, off_skip, off_lens, off_meta, off_table, off_out, off_lse, off_part_o, off_part_ml, total;
+    SharedAttnSlots slots;
+    size_t off_o, off_ml, off_meta, off_seqs, off_groups, total;
 };
 
 SharedLayout shared_layout(const massv_attn_desc& d, int n_groups) {
     SharedLayout l;
-    l.attn = attn_layout(d);
-    const size_t B = d.batch, rows = B * (d.gamma + 1) * d.n_q_heads;
-    l.slot_tiles = shared_attn_slot_tiles(d.head_dim, (long)(rows / d.n_kv_heads));
-    size_t off = align_up(l.attn.total, kAlign);
+    l.slots = shared_attn_slots(d.batch, d.gamma + 1, d.n_q_heads, d.n_kv_heads, d.head_dim, n_groups);
+    size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += align_up(bytes, kAlign); return at; };
-    l.off_groups = take((size_t)n_groups * sizeof(int4));
-    l.off_skip = take(B * sizeof(int32_t));
-    l.off_lens = take(B * sizeof(int32_t));
-    l.off_meta = take((size_t)(n_groups + 2) * sizeof(int32_t));
-    l.off_table = take(B * d.max_pages_per_seq * sizeof(int32_t));
-    l.off_out = take(rows * d.head_dim * sizeof(float));
-    l.off_lse = take(rows * sizeof(float));
-    const size_t slots = (size_t)2 * kPrefixMaxCtas * l.slot_tiles * 128;
-    l.off_part_o = take(slots * d.head_dim * sizeof(float));
-    l.off_part_ml = take(slots * 2 * sizeof(float));
+    l.off_o = take(l.slots.rows() * d.head_dim * sizeof(float));
+    l.off_ml = take(l.slots.rows() * 2 * sizeof(float));
+    l.off_meta = take(2 * sizeof(int32_t));
+    l.off_seqs = take((size_t)d.batch * sizeof(int4));
+    l.off_groups = take((size_t)d.batch * sizeof(int4));
     l.total = off;
     return l;
 }
@@ -157,10 +148,10 @@ int check_shared(const massv_attn_desc* d, int32_t n_groups) {
     const int rc = check_attn_desc(d);
     if (rc != MASSV_OK) return rc;
     if (n_groups < 1) return MASSV_ERR_INVALID_ARG;
-    if (n_groups > kMaxGroups || d->window != 0) return MASSV_ERR_UNSUPPORTED;
-    // the prefix kernel counts (tile, KV head, block) products of all groups in 32 bits
-    const double pairs = 128 / (d->n_q_heads / d->n_kv_heads), tiles = (double)d->batch * (d->gamma + 1) / pairs + n_groups;
-    if (tiles * d->n_kv_heads * ((double)d->max_pages_per_seq * kPageSize / kPrefixBlock) > 1e9) return MASSV_ERR_UNSUPPORTED;
+    if (n_groups > kMaxGroups || d->batch > kSharedMaxBatch || d->window != 0) return MASSV_ERR_UNSUPPORTED;
+    // the kernel counts the cost of all blocks in 32 bits
+    const double pairs = 128 / (d->n_q_heads / d->n_kv_heads), tiles = (double)d->batch * (d->gamma + 1) / pairs + n_groups + d->batch;
+    if (tiles * d->n_kv_heads * ((double)d->max_pages_per_seq * kPageSize / kPrefixBlock + 1) > 2e8) return MASSV_ERR_UNSUPPORTED;
     return MASSV_OK;
 }
 
@@ -249,21 +240,15 @@ int massv_verify_attn_shared(const massv_attn_desc* desc, int32_t n_groups, cons
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0 || workspace_bytes < l.total) return MASSV_ERR_WORKSPACE;
     char* ws = static_cast<char*>(workspace);
     SharedAttnParams p;
-    p.a = attn_params(desc, l.attn, q, k_new, v_new, k_pages, v_pages, page_table, seq_lens, out, out_f32, lse, ws, dev_status);
+    p.a = attn_params(desc, AttnLayout{}, q, k_new, v_new, k_pages, v_pages, page_table, seq_lens, out, out_f32, lse, nullptr, dev_status);
     p.n_groups = n_groups; p.group_start = group_start; p.shared_lens = shared_lens;
-    p.groups = reinterpret_cast<int4*>(ws + l.off_groups);
-    p.skip = reinterpret_cast<int32_t*>(ws + l.off_skip);
-    p.tail_lens = reinterpret_cast<int32_t*>(ws + l.off_lens);
-    p.tail_table = reinterpret_cast<int32_t*>(ws + l.off_table);
-    // sequences that share nothing are finished by the kernels of the rest: they write the caller's buffers where there are any
-    p.tail_out = out_f32 ? out_f32 : reinterpret_cast<float*>(ws + l.off_out);
-    p.tail_lse = lse ? lse : reinterpret_cast<float*>(ws + l.off_lse);
+    p.slots = l.slots;
+    p.part_o = reinterpret_cast<float*>(ws + l.off_o);
+    p.part_ml = reinterpret_cast<float*>(ws + l.off_ml);
     p.meta = reinterpret_cast<int32_t*>(ws + l.off_meta);
-    p.slot_tiles = l.slot_tiles;
-    p.part_o = reinterpret_cast<float*>(ws + l.off_part_o);
-    p.part_ml = reinterpret_cast<float*>(ws + l.off_part_ml);
-    const AttnParams rest = attn_params(desc, l.attn, q, k_new, v_new, k_pages, v_pages, p.tail_table, p.tail_lens, out, p.tail_out, p.tail_lse, ws, dev_status);
-    return launch_shared_attn(p, rest, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
+    p.seqs = reinterpret_cast<int4*>(ws + l.off_seqs);
+    p.seq_groups = reinterpret_cast<int4*>(ws + l.off_groups);
+    return launch_shared_attn(p, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
 }
 
 size_t massv_accept_workspace_size(const massv_accept_desc* desc) {

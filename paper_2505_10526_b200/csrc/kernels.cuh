@@ -49,24 +49,28 @@ cudaError_t launch_attn_umma(const AttnParams& p, const CUtensorMap& map_k, cons
                              int* launched, cudaEvent_t split_done);
 
 // ---------------------------------------------------------------- attention over a shared prefix
-constexpr int kPrefixBlock = 128;      // positions of a block of the prefix
+constexpr int kPrefixBlock = 128;      // positions of a block
 constexpr int kMaxGroups = 256;
-constexpr int kPrefixMaxCtas = 160;    // resident CTAs of the prefix kernel, one per SM
+constexpr int kSharedMaxBatch = 2048;
+constexpr int kSharedMaxCtas = 160;    // resident CTAs, one per SM
+// Slots for pieces: tiles each, of 128 rows, or tail_rows for the last kind.
+struct SharedAttnSlots {
+    int tiles, tail_rows, cut, prefix_items, tails;
+    __host__ __device__ size_t rows() const { return (size_t)(cut + prefix_items) * tiles * 128 + (size_t)tails * tiles * tail_rows; }
+};
 struct SharedAttnParams {
-    AttnParams a;                      // the call as it stands: queries, pools, the caller's page tables and lengths, outputs
+    AttnParams a;                      // the call as massv_verify_attn takes it; its scratch is not used
     int n_groups;
     const int32_t *group_start, *shared_lens;
-    int4* groups;                      // [n_groups] blocks of the shared prefix, the sequence whose table is read, first (sequence, row) pair, pairs
-    int32_t* skip;                     // [B] positions that the prefix kernel covers
-    int32_t *tail_lens, *tail_table;   // [B], [B, max_pages]: lengths and tables behind them
-    float *tail_out, *tail_lse;        // [B, R, Hq, d], [B, R, Hq]: the rest's result (the caller's out_f32 and lse where they are given)
-    int32_t* meta;                     // [0] units per CTA, [1 + g] units of groups 0 .. g-1
-    int slot_tiles;                    // tiles a slot has room for
-    float *part_o, *part_ml;           // [2 * kPrefixMaxCtas, slot_tiles, 128, d], [.., 128, 2]: pieces
+    SharedAttnSlots slots;
+    float *part_o, *part_ml;           // [slots.rows(), d], [slots.rows(), 2]: pieces
+    // for the merge
+    int32_t* meta;                     // [0] cost of a range, [1] cost of all prefix items
+    int4* seqs;                        // [B] tail blocks of earlier sequences (per KV head), own, first pair within the group, blocks of its prefix
+    int4* seq_groups;                  // [B] cost of earlier groups, their items, cost of a block of the group
 };
-int shared_attn_slot_tiles(int d, long rows);      // rows: query rows of all sequences per KV head
-// rest: the same call on tail_table, tail_lens, tail_out and tail_lse
-cudaError_t launch_shared_attn(const SharedAttnParams& p, const AttnParams& rest, cudaStream_t stream);
+SharedAttnSlots shared_attn_slots(int B, int R, int Hq, int Hkv, int d, int n_groups);
+cudaError_t launch_shared_attn(const SharedAttnParams& p, cudaStream_t stream);
 
 // ---------------------------------------------------------------- LM head
 struct LmHeadParams {

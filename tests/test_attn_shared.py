@@ -26,7 +26,7 @@ def test_refusals(mv):
     assert call(mv.attn_desc(4, 9, 8, 2, 64, 20, 100)) == -2 and call(mv.attn_desc(4, 3, 8, 3, 64, 20, 100)) == -2
     assert call(d, ws=None) == -4 and call(d, ws=a + 16) == -4 and call(d, n=1000) == -4
     size = mv.massv_verify_attn_shared_workspace_size
-    assert size(d, 1) > mv.massv_verify_attn_workspace_size(d) and size(d, 0) == 0 and size(d, 257) == 0 and size(mv.attn_desc(4, 3, 8, 2, 64, 20, 100, window=1), 1) == 0
+    assert size(d, 1) > 0 and size(mv.attn_desc(2049, 3, 8, 2, 64, 20, 100), 1) == 0 and size(d, 0) == 0 and size(d, 257) == 0 and size(mv.attn_desc(4, 3, 8, 2, 64, 20, 100, window=1), 1) == 0
     i, b = torch.zeros(2, dtype=torch.int32), torch.zeros(64, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="CUDA device"):
         mv.massv_verify_attn_shared(d, i, i[:1], b, b, b, b, b, i, i, b)

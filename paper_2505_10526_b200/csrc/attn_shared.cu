@@ -14,11 +14,12 @@
 // PREFIX items: a tile is as many whole (sequence, block row) pairs of a KV head's G query heads as fit 128 rows.  At head_dim 64 and
 // 128 a CTA works on two tiles at once, so that one tile's products run under the other's exponentials; both share each K and V
 // block.  At 256 the accumulator leaves room for one, whose scores are double buffered instead.  Every position is seen by every row.
-// TAIL items: the positions of one sequence behind the prefix, block rows included (appended here), for its G * R <= 64 rows.  With room
-// for two tiles, even and odd blocks go to one accumulator each, which keeps two blocks in flight.
+// TAIL items: the positions of one sequence behind the prefix, block rows included (appended here), for its G * R <= 64 rows.  The
+// blocks of all tails of a CTA form one pipeline across items (the next item's queries have a buffer of their own): the scores run two
+// blocks ahead of the weights, and where there is room for two accumulators the blocks alternate between them.
 //
-// Warp 0 copies (TMA), one thread of warp 1 issues the products, warp 2 patches the block's own K/V rows into the blocks that hold their
-// positions and stores them to their page slots, four warps per tile make the softmax.
+// Warps 0 and 3 copy K and V (TMA), each into a ring of its own; warp 1 issues the products; warp 2 patches the block's own K/V rows into
+// the blocks that hold their positions and stores them to their page slots; four warps per tile make the softmax.
 //
 // All items form one line, a block costing what its kind costs (below), cut into equal ranges for a persistent grid of one CTA per
 // SM: prefix items, which the tensor cores bound, and tails, which memory bounds, are at work at the same time.  What a CTA has
@@ -35,8 +36,16 @@ constexpr int kTileRows = 128;
 constexpr int kPagesPerBlock = kPrefixBlock / kPageSize;
 constexpr float kRescaleThreshold = 8.f;   // log2 units a row's maximum may outgrow its reference by
 
-// Cost of a block: products of two tiles, of one, of a tail.
-constexpr int kCostTwo = 8, kCostOne = 5, kCostTail = 4;
+// Cost of a block: products of two tiles, of one, of a tail; and what an item costs beside its blocks (queries, write-out).
+constexpr int kCostTwo = 8, kCostOne = 5, kCostTail = 4, kCostPrefixItem = 8, kCostTailItem = 4;
+constexpr int kCostMost = kCostTwo + kCostPrefixItem;
+
+// Blocks of an item that begins at `start`: block 0 there, block k > 0 at start + item + k * block.  The first block that begins at or
+// behind position f of the line (n or more: none).
+__device__ __forceinline__ int first_block(int f, int start, int block, int item) {
+    return f <= start ? 0 : max(1, (f - start - item + block - 1) / block);
+}
+__device__ __forceinline__ int block_begin(int k, int start, int block, int item) { return k == 0 ? start : start + item + k * block; }
 
 template <int D>
 struct SharedCfg {
@@ -45,9 +54,9 @@ struct SharedCfg {
     static constexpr int kNCH = D / 64;
     static constexpr int kQTile = kTileRows * D * 2;
     static constexpr int kEntry = kPrefixBlock * D * 2 / kParts;
-    static constexpr int kEntries = D == 64 ? 8 : 4;
+    static constexpr int kEntries = D == 64 ? 4 : 2;         // of each ring
     static constexpr int kBoxes = kPagesPerBlock * kNCH / kParts;      // 16-position x 64-element boxes of an entry
-    static constexpr int kSmem = kTiles * kQTile + kEntries * kEntry + 1024;      // and the line (line_ints)
+    static constexpr int kSmem = kTiles * kQTile + 2 * kEntries * kEntry + 1024;      // and the line (line_ints)
     static constexpr int kThreads = 128 + kTiles * 128;
     static constexpr uint32_t kTmemCols = 512;
     static constexpr uint32_t kTmemO = 2 * kPrefixBlock;      // two score buffers, then the accumulators
@@ -121,7 +130,7 @@ struct Line {
     const int* gitem;     // [n_groups + 1] their number
     const int* gblocks;   // [n_groups] blocks of the shared prefix
     const int* gsrc;      // [n_groups] the sequence whose page table is read for it
-    const int* tail;      // [B + 1] tail blocks of sequences 0 .. b-1, per KV head
+    const int* tail;      // [B + 1] cost of the tails of sequences 0 .. b-1, per KV head
     int n_groups, B;
 };
 __device__ __forceinline__ int find_last(const int* cum, int n, int u) {       // the largest i < n with cum[i] <= u
@@ -148,14 +157,15 @@ struct Run {
 template <int D>
 __global__ void __launch_bounds__(SharedCfg<D>::kThreads, 1)
 attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q,
-                   const SharedAttnParams p) {
+                   const __grid_constant__ CUtensorMap map_qt, const SharedAttnParams p) {
     using Cfg = SharedCfg<D>;
     constexpr int E = Cfg::kEntries, NT = Cfg::kTiles, PARTS = Cfg::kParts, NCH = Cfg::kNCH;
     constexpr int UPR = D / 8;             // 16-byte units per K/V row
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t ready_bar[E], empty_bar[E];
-    __shared__ __align__(8) uint64_t landed_bar[E];                    // the bytes of an entry that still needs patching
-    __shared__ __align__(8) uint64_t q_ready_bar, q_free_bar;
+    // rings: K's entries, then V's
+    __shared__ __align__(8) uint64_t ready_bar[2 * E], empty_bar[2 * E];
+    __shared__ __align__(8) uint64_t landed_bar[2 * E];                // the bytes of an entry that still needs patching
+    __shared__ __align__(8) uint64_t q_ready_bar[2], q_free_bar[2];   // by query buffer: a prefix item has both, tails take turns
     __shared__ __align__(8) uint64_t s_full_bar[2], p_full_bar[2];     // by score buffer
     __shared__ __align__(8) uint64_t o_full_bar[2], o_free_bar[2];     // by tile
     __shared__ __align__(8) uint64_t pv_done_bar;                      // one tile: O is up to date
@@ -166,9 +176,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const int R = p.a.R, B = p.a.B, cap = p.a.max_pages * kPageSize;
     const int G = p.a.Hq / p.a.Hkv, nb = kTileRows / G, tile_rows = nb * G;
     if (threadIdx.x == 0) {
-        for (int e = 0; e < E; ++e) { mbar_init(&ready_bar[e], 1); mbar_init(&empty_bar[e], 1); mbar_init(&landed_bar[e], 1); }
-        mbar_init(&q_ready_bar, 1); mbar_init(&q_free_bar, 1); mbar_init(&pv_done_bar, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full_bar[i], 1); mbar_init(&p_full_bar[i], 4); mbar_init(&o_full_bar[i], 1); mbar_init(&o_free_bar[i], 4); }
+        for (int e = 0; e < 2 * E; ++e) { mbar_init(&ready_bar[e], 1); mbar_init(&empty_bar[e], 1); mbar_init(&landed_bar[e], 1); }
+        mbar_init(&pv_done_bar, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(&q_ready_bar[i], 1); mbar_init(&q_free_bar[i], 1); mbar_init(&s_full_bar[i], 1); mbar_init(&p_full_bar[i], 4); mbar_init(&o_full_bar[i], 1); mbar_init(&o_free_bar[i], 4); }
         abort_flag = 0;
         s_bad = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -179,8 +189,12 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t* q_smem = smem + E * Cfg::kEntry;                          // [tile][d / 64][128 rows][128 B], swizzled
-    int* gs = reinterpret_cast<int*>(q_smem + NT * Cfg::kQTile);
+    uint8_t* q_smem = smem;                                            // [tile][d / 64][128 rows][128 B], swizzled
+    // Where a tail's queries go: a tile's place each, or (one tile) the two halves of its rows.  A product of 128 rows from the
+    // second half on reads 64 rows of what stands behind it: rows nobody takes.
+    constexpr int kQTurn = NT == 2 ? Cfg::kQTile : 64 * 128;
+    uint8_t* ring_smem = q_smem + NT * Cfg::kQTile;
+    int* gs = reinterpret_cast<int*>(ring_smem + 2 * E * Cfg::kEntry);
     int *gcost = gs + p.n_groups + 1, *gitem = gcost + p.n_groups + 1, *gblocks = gitem + p.n_groups + 1, *gsrc = gblocks + p.n_groups, *tail = gsrc + p.n_groups;
     const Line ln{gs, gcost, gitem, gblocks, gsrc, tail, p.n_groups, B};
     // rows past the last pair of a tile are never copied
@@ -224,12 +238,12 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const int L = tail[b + 1];
         const bool ok = fits(L);
         if (!ok && blockIdx.x == 0) set_status(p.a.dev_status, MASSV_ERR_CAPACITY);
-        tail[b + 1] = ok ? (L + R + kPrefixBlock - 1) / kPrefixBlock - gblocks[find_last(gs, p.n_groups, b)] : 0;
+        tail[b + 1] = ok ? ((L + R + kPrefixBlock - 1) / kPrefixBlock - gblocks[find_last(gs, p.n_groups, b)]) * kCostTail + kCostTailItem : 0;
     }
     for (int i = threadIdx.x; i < p.n_groups; i += blockDim.x) {
         const int pairs = (gs[i + 1] - gs[i]) * R, tiles = (pairs + nb - 1) / nb, items = gblocks[i] > 0 ? (tiles + NT - 1) / NT * p.a.Hkv : 0;
         gitem[i + 1] = items;
-        gcost[i + 1] = items * gblocks[i] * (NT == 2 && tiles > 1 ? kCostTwo : kCostOne);
+        gcost[i + 1] = items * (gblocks[i] * (NT == 2 && tiles > 1 ? kCostTwo : kCostOne) + kCostPrefixItem);
     }
     if (threadIdx.x == 0) { gcost[0] = 0; gitem[0] = 0; tail[0] = 0; }
     tc_fence_before();
@@ -253,8 +267,8 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     else if (warp == 3) scan(tail, B);
     __syncthreads();
     const int tails0 = gcost[p.n_groups];                              // where the tails begin on the line
-    const int total = tails0 + tail[B] * p.a.Hkv * kCostTail;
-    const int per = max(kCostTwo, (total + (int)gridDim.x - 1) / (int)gridDim.x);        // (no block is longer than a range)
+    const int total = tails0 + tail[B] * p.a.Hkv;
+    const int per = max(kCostMost, (total + (int)gridDim.x - 1) / (int)gridDim.x);       // (no block is longer than a range)
     if (blockIdx.x == 0) {
         if (threadIdx.x == 0) {
             p.meta[0] = per; p.meta[1] = tails0;
@@ -262,24 +276,24 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
         for (int b = threadIdx.x; b < B; b += blockDim.x) {
             const int g = find_last(gs, p.n_groups, b);
-            p.seqs[b] = make_int4(tail[b], tail[b + 1] - tail[b], (b - gs[g]) * R, gblocks[g]);
+            p.seqs[b] = make_int4(tail[b], (tail[b + 1] - tail[b] - kCostTailItem) / kCostTail, (b - gs[g]) * R, gblocks[g]);
             p.seq_groups[b] = make_int4(gcost[g], gitem[g], NT == 2 && (gs[g + 1] - gs[g]) * R > nb ? kCostTwo : kCostOne, 0);
         }
     }
 
     // ---- this CTA's range: the blocks that begin in it
     const int f_begin = min((long long)total, (long long)blockIdx.x * per), f_end = min((long long)total, (long long)f_begin + per);
-    int f = f_begin;
-    // The item that position f of the line lies in, and the run of its blocks that begin at or behind f and inside the range.
-    auto next_run = [&](Run& r) -> bool {
+    // The blocks at or behind f of the item that position f of the line lies in (or of the next one), and f behind them.
+    auto next_run = [&](int& f, Run& r) -> bool {
         while (f < f_end) {
-            int start, n_all, cost, item;
+            int start, n_all, cost, extra, item;
             if (f < tails0) {
                 const int g = find_last(ln.gcost, ln.n_groups, f), pairs = (ln.gs[g + 1] - ln.gs[g]) * R;
                 cost = NT == 2 && pairs > nb ? kCostTwo : kCostOne;
+                extra = kCostPrefixItem;
                 n_all = ln.gblocks[g];
-                const int k = (f - ln.gcost[g]) / (n_all * cost), tile = k / p.a.Hkv, done = tile * nb * NT;
-                start = ln.gcost[g] + k * n_all * cost;
+                const int length = n_all * cost + extra, k = (f - ln.gcost[g]) / length, tile = k / p.a.Hkv, done = tile * nb * NT;
+                start = ln.gcost[g] + k * length;
                 item = ln.gitem[g] + k;
                 r.tail = false;
                 r.head = k - tile * p.a.Hkv;
@@ -288,100 +302,94 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 r.n_rows[0] = min(nb, pairs - done) * G;
                 r.n_rows[1] = NT == 2 ? max(0, min(nb, pairs - done - nb)) * G : 0;
                 r.pos0 = 0;
+                r.L = 0;
             } else {
-                const int u = (f - tails0) / kCostTail, b = find_last(ln.tail, B, u / p.a.Hkv);      // (blocks of a sequence: n per head, head after head)
+                const int u = f - tails0, b = find_last(ln.tail, B, u / p.a.Hkv), length = ln.tail[b + 1] - ln.tail[b];      // (head after head)
                 cost = kCostTail;
-                n_all = ln.tail[b + 1] - ln.tail[b];
-                r.head = (u - ln.tail[b] * p.a.Hkv) / n_all;
-                start = tails0 + (ln.tail[b] * p.a.Hkv + r.head * n_all) * kCostTail;
+                extra = kCostTailItem;
+                n_all = (length - extra) / cost;
+                r.head = (u - ln.tail[b] * p.a.Hkv) / length;
+                start = tails0 + ln.tail[b] * p.a.Hkv + r.head * length;
                 item = p.slots.prefix_items + b * p.a.Hkv + r.head;
                 r.tail = true;
                 r.seq = b;
                 r.blk0 = b * R;
                 r.n_rows[0] = r.n_rows[1] = R * G;
                 r.pos0 = ln.gblocks[find_last(ln.gs, ln.n_groups, b)] * kPrefixBlock;
+                r.L = p.a.seq_lens[b];
             }
-            const int k0 = (f - start + cost - 1) / cost, k1 = min(n_all, (f_end - start + cost - 1) / cost);
-            f = start + k1 * cost;
+            const int k0 = first_block(f, start, cost, extra), k1 = min(n_all, first_block(f_end, start, cost, extra));
+            f = k1 == n_all ? start + extra + n_all * cost : f_end;
             if (k0 >= k1) continue;         // the item's last block begins ahead of the range
             r.pos0 += k0 * kPrefixBlock;
             r.n = k1 - k0;
             // an item that began in an earlier CTA's range has slot 0, one that runs on into the next has slot 1
             r.slot = k0 == 0 && k1 == n_all ? -1 - item : (int)blockIdx.x * 2 + (k0 > 0 ? 0 : 1);
-            r.L = r.tail ? p.a.seq_lens[r.seq] : 0;
-            if (r.tail && (NT == 1 || r.n < 2)) r.n_rows[1] = 0;
             return true;
         }
         return false;
     };
-    // Entries of the ring are filled in the order in which the products take them.  Two tiles on one prefix: K0 V0 K1 V1 ...; otherwise
-    // the scores run a block ahead: K0 K1 V0 K2 V1 ... V(n-1).
-    auto decode = [&](const Run& r, int i, int& t, int& is_v) {
-        if (NT == 2 && !r.tail) { t = i >> 1; is_v = i & 1; }
-        else if (i == 0) { t = 0; is_v = 0; }
-        else if (i == 2 * r.n - 1) { t = r.n - 1; is_v = 1; }
-        else if (i & 1) { t = (i + 1) >> 1; is_v = 0; }
-        else { t = (i >> 1) - 1; is_v = 1; }
-    };
+    // Two tiles on one prefix; everything else is one pipeline over all blocks, in which the scores run two blocks ahead.
+    auto paired = [&](const Run& r) { return NT == 2 && !r.tail; };
 
-    const uint32_t tmem_base = tmem_base_slot;
+    constexpr uint32_t tmem_base = 0;                                  // all 512 columns are this CTA's: they begin at 0
     volatile int* abort_ptr = &abort_flag;
-    Run r;
-    if (warp == 0) {
-        // ------------------------------------------------ copies
+    if (warp == 0 || warp == 3) {
+        // ------------------------------------------------ copies: K (and the queries) by warp 0, V by warp 3
+        const bool is_v = warp == 3;
         uint64_t policy;
         asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
-        int it = 0;                      // entries filled so far
+        // This lane's 16-position x 64-element box of an entry: K parts are halves of d, V parts halves of the positions.
+        const int groups = is_v ? NCH : NCH / PARTS, pages = Cfg::kBoxes / groups;
+        const int c = lane % groups, pg = lane / groups, box = c * (pages * kPageSize * 128) + pg * 2048;
+        const CUtensorMap* map = is_v ? &map_v : &map_k;
+        uint8_t* ring = ring_smem + (is_v ? E * Cfg::kEntry : 0);
+        uint64_t *ready = ready_bar + (is_v ? E : 0), *landed = landed_bar + (is_v ? E : 0), *empty = empty_bar + (is_v ? E : 0);
+        int f = f_begin, e = 0, turn = 0;          // ring entry; tails so far
+        uint32_t lap = 1;                          // parity to wait for: an entry's first use does not wait
+        int q_uses[2] = {0, 0};
         bool ok = true;
-        for (int run = 0; ok && next_run(r); ++run) {
-            if (run >= 1) {
-                int fr = 0;
-                if (lane == 0) fr = mbar_wait(&q_free_bar, (uint32_t)(run - 1) & 1u, abort_ptr) ? 1 : 0;
-                if (!__shfl_sync(0xffffffffu, fr, 0)) { ok = false; break; }
-            }
-            const int tiles = !r.tail && r.n_rows[1] > 0 ? 2 : 1;      // (a tail's two accumulators have the same rows)
-            if (lane == 0) mbar_expect_tx(&q_ready_bar, (uint32_t)(tiles * tile_rows * D * 2));
-            __syncwarp();
-            if (lane < tiles * NCH) {
-                const int x = lane / NCH, dc = lane % NCH;
-                tma_load_3d(q_smem + x * Cfg::kQTile + dc * (kTileRows * 128), &map_q, dc * 64, r.head * G, r.blk0 + x * nb, &q_ready_bar, policy);
+        Run r;
+        while (ok && next_run(f, r)) {
+            if (!is_v) {
+                const int buf = r.tail ? turn++ & 1 : 0, used = buf ? q_uses[1]++ : q_uses[0]++;
+                if (used > 0 && !mbar_wait_warp(&q_free_bar[buf], (uint32_t)(used - 1) & 1u, abort_ptr)) break;
+                const int tiles = !r.tail && r.n_rows[1] > 0 ? 2 : 1;
+                if (lane == 0) mbar_expect_tx(&q_ready_bar[buf], (uint32_t)(tiles * (r.tail ? R * G : tile_rows) * D * 2));
+                __syncwarp();
+                if (lane < tiles * NCH) {
+                    const int x = lane / NCH, dc = lane % NCH;
+                    uint8_t* dst = q_smem + dc * (kTileRows * 128);
+                    if (r.tail) tma_load_3d(dst + buf * kQTurn, &map_qt, dc * 64, r.head * G, r.blk0, &q_ready_bar[buf], policy);
+                    else tma_load_3d(dst + x * Cfg::kQTile, &map_q, dc * 64, r.head * G, r.blk0 + x * nb, &q_ready_bar[buf], policy);
+                }
             }
             // page ids travel in registers: lane l holds page 32 * group + l of the run, four blocks to a group
             const int32_t* pt = p.a.page_table + (size_t)r.seq * p.a.max_pages + r.pos0 / kPageSize;
             const int end = r.tail ? min(r.L + R - r.pos0, r.n * kPrefixBlock) : r.n * kPrefixBlock;      // positions of the run
             const int n_pages = (end + kPageSize - 1) / kPageSize;
-            int pid_prev = 0, pid_cur = lane < n_pages ? pt[lane] : 0, pid_next = 32 + lane < n_pages ? pt[32 + lane] : 0, grp = 0;
-            for (int i = 0; i < 2 * r.n && ok; ++i) {
-                int t, is_v;
-                decode(r, i, t, is_v);
-                if (t / 4 > grp) {       // only a K block can be the first of a new group
-                    grp = t / 4;
-                    pid_prev = pid_cur; pid_cur = pid_next;
-                    const int nxt = (grp + 1) * 32 + lane;
+            int pid_cur = lane < n_pages ? pt[lane] : 0, pid_next = 32 + lane < n_pages ? pt[32 + lane] : 0;
+            for (int t = 0; t < r.n && ok; ++t) {
+                if (t > 0 && t % 4 == 0) {
+                    pid_cur = pid_next;
+                    const int nxt = (t / 4 + 1) * 32 + lane;
                     pid_next = nxt < n_pages ? pt[nxt] : 0;
                 }
-                const int held = t / 4 == grp ? pid_cur : pid_prev;
                 const bool patch = r.tail && r.pos0 + (t + 1) * kPrefixBlock > r.L;
                 const int have = min(kPagesPerBlock, n_pages - t * kPagesPerBlock);        // pages of the block that hold positions
-                for (int part = 0; part < PARTS; ++part, ++it) {
-                    const int e = it % E;
-                    int freed = 0;
-                    if (lane == 0) freed = mbar_wait(&empty_bar[e], (((uint32_t)(it / E)) & 1u) ^ 1u, abort_ptr) ? 1 : 0;
-                    if (!__shfl_sync(0xffffffffu, freed, 0)) { ok = false; break; }
-                    // K parts are halves of d, V parts halves of the positions
-                    const int groups = is_v ? NCH : NCH / PARTS, pages = Cfg::kBoxes / groups;
-                    const int c = lane % groups, pg = lane / groups;
-                    const int dc = is_v ? c : part * groups + c, page0 = is_v ? part * pages : 0;
-                    const int n_pg = max(0, min(pages, have - page0));
-                    uint64_t* bar = patch ? &landed_bar[e] : &ready_bar[e];
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                    const int page0 = is_v ? part * pages : 0, n_pg = max(0, min(pages, have - page0));
+                    int pid = __shfl_sync(0xffffffffu, pid_cur, (t % 4) * kPagesPerBlock + (page0 + pg) % kPagesPerBlock);
+                    if (!mbar_wait_warp(&empty[e], lap, abort_ptr)) { ok = false; break; }
+                    uint64_t* bar = patch ? &landed[e] : &ready[e];
                     if (lane == 0) mbar_expect_tx(bar, (uint32_t)(n_pg * groups * 2048));
                     __syncwarp();
-                    int pid = __shfl_sync(0xffffffffu, held, (t % 4) * kPagesPerBlock + (page0 + pg) % kPagesPerBlock);
                     if (lane < Cfg::kBoxes && pg < n_pg) {
                         if (pid < 0 || pid >= p.a.num_pages) { set_status(p.a.dev_status, MASSV_ERR_CAPACITY); pid = 0; }
-                        tma_load_2d(smem + (size_t)e * Cfg::kEntry + c * (pages * kPageSize * 128) + pg * 2048, is_v ? &map_v : &map_k, dc * 64,
-                                    (pid * p.a.Hkv + r.head) * kPageSize, bar, policy);
+                        tma_load_2d(ring + e * Cfg::kEntry + box, map, (is_v ? c : part * groups + c) * 64, (pid * p.a.Hkv + r.head) * kPageSize, bar, policy);
                     }
+                    if (++e == E) { e = 0; lap ^= 1u; }
                 }
             }
         }
@@ -391,186 +399,193 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     } else if (warp == 2) {
         // ------------------------------------------------ helper: the block's own rows, and what lies behind the last position
         uint32_t landed_phase = 0;       // bit e: parity of the next completion of landed_bar[e]
-        int it0 = 0;                     // entries of earlier runs
+        int ring_at[2] = {0, 0};         // entries of each ring so far
         bool ok = true;
-        for (; ok && next_run(r); it0 += 2 * r.n * PARTS) {
-            if (!r.tail || r.pos0 + r.n * kPrefixBlock <= r.L) continue;
-            const int t_first = max(0, r.L - r.pos0) / kPrefixBlock, end = r.L + R;
+        // One block's K or V, entry by entry.
+        auto patch = [&](const Run& r, int t, bool is_v) {
+            const int start = r.pos0 + t * kPrefixBlock, end = r.L + R;
+            int& it = ring_at[is_v ? 1 : 0];
+            if (!r.tail || start + kPrefixBlock <= r.L) { it += PARTS; return; }
             const int32_t* pt = p.a.page_table + (size_t)r.seq * p.a.max_pages;
-            for (int i = 0; i < 2 * r.n && ok; ++i) {
-                int t, is_v;
-                decode(r, i, t, is_v);
-                if (t < t_first) continue;
-                const int start = r.pos0 + t * kPrefixBlock;
-                const __nv_bfloat16* src = is_v ? p.a.v_new : p.a.k_new;
-                __nv_bfloat16* pool = is_v ? p.a.v_pages : p.a.k_pages;
-                for (int part = 0; part < PARTS; ++part) {
-                    const int e = (it0 + i * PARTS + part) % E;
-                    // the entry's positions and 16-byte units of a row: K parts are halves of d, V parts halves of the positions
-                    constexpr int kVRows = kPrefixBlock / PARTS, kKUnits = UPR / PARTS;
-                    const int row0 = is_v ? part * kVRows : 0, n_row = is_v ? kVRows : kPrefixBlock, u0 = is_v ? 0 : part * kKUnits, n_u = is_v ? UPR : kKUnits;
-                    const int first = max(r.L, start + row0), last = min(end, start + row0 + n_row);      // new positions inside
-                    uint8_t* dst = smem + (size_t)e * Cfg::kEntry;
-                    auto at = [&](int row, int u) { const int w = row - row0; return dst + (u / 8) * (n_row * 128) + w * 128 + (((u % 8) ^ (w & 7)) << 4); };
-                    // what comes from memory is asked for ahead of the wait
-                    constexpr int PRE = 4;
-                    const int n_units = max(0, last - first) * n_u;
-                    uint4 val[PRE];
-                    int pid[PRE];
+            const __nv_bfloat16* src = is_v ? p.a.v_new : p.a.k_new;
+            __nv_bfloat16* pool = is_v ? p.a.v_pages : p.a.k_pages;
+            for (int part = 0; part < PARTS; ++part, ++it) {
+                const int e = it % E + (is_v ? E : 0);
+                // the entry's positions and 16-byte units of a row: K parts are halves of d, V parts halves of the positions
+                constexpr int kVRows = kPrefixBlock / PARTS, kKUnits = UPR / PARTS;
+                const int row0 = is_v ? part * kVRows : 0, n_row = is_v ? kVRows : kPrefixBlock, u0 = is_v ? 0 : part * kKUnits, n_u = is_v ? UPR : kKUnits;
+                const int first = max(r.L, start + row0), last = min(end, start + row0 + n_row);      // new positions inside
+                uint8_t* dst = ring_smem + (size_t)e * Cfg::kEntry;
+                auto at = [&](int row, int u) { const int w = row - row0; return dst + (u / 8) * (n_row * 128) + w * 128 + (((u % 8) ^ (w & 7)) << 4); };
+                // what comes from memory is asked for ahead of the wait
+                constexpr int PRE = 4;
+                const int n_units = max(0, last - first) * n_u;
+                uint4 val[PRE];
+                int pid[PRE];
 #pragma unroll
-                    for (int k = 0; k < PRE; ++k) {
-                        const int idx = k * 32 + lane;
-                        if (idx < n_units) {
-                            const int pos = first + idx / n_u, u = u0 + idx % n_u;
-                            val[k] = *reinterpret_cast<const uint4*>(src + (((size_t)r.seq * R + (pos - r.L)) * p.a.Hkv + r.head) * D + u * 8);
-                            pid[k] = pt[pos / kPageSize];
-                        }
-                    }
-                    if (!mbar_wait_warp(&landed_bar[e], (landed_phase >> e) & 1u, abort_ptr)) { ok = false; break; }
-                    landed_phase ^= 1u << e;
-                    auto put = [&](int idx, const uint4& x, int page) {
+                for (int k = 0; k < PRE; ++k) {
+                    const int idx = k * 32 + lane;
+                    if (idx < n_units) {
                         const int pos = first + idx / n_u, u = u0 + idx % n_u;
-                        *reinterpret_cast<uint4*>(at(pos - start, u - u0)) = x;
-                        if (page >= 0 && page < p.a.num_pages)
-                            *reinterpret_cast<uint4*>(pool + (((size_t)page * p.a.Hkv + r.head) * kPageSize + (pos % kPageSize)) * D + u * 8) = x;
-                    };
-#pragma unroll
-                    for (int k = 0; k < PRE; ++k)
-                        if (k * 32 + lane < n_units) put(k * 32 + lane, val[k], pid[k]);
-                    for (int idx = PRE * 32 + lane; idx < n_units; idx += 32) {
-                        const int pos = first + idx / n_u, u = u0 + idx % n_u;
-                        put(idx, *reinterpret_cast<const uint4*>(src + (((size_t)r.seq * R + (pos - r.L)) * p.a.Hkv + r.head) * D + u * 8), pt[pos / kPageSize]);
+                        val[k] = *reinterpret_cast<const uint4*>(src + (((size_t)r.seq * R + (pos - r.L)) * p.a.Hkv + r.head) * D + u * 8);
+                        pid[k] = pt[pos / kPageSize];
                     }
-                    if (is_v) {
-                        // positions past the end have weight zero, but zero times a stale NaN would still poison P V
-                        const int z0 = max(row0, end - start), n_zero = row0 + n_row - z0;
-                        for (int idx = lane; idx < n_zero * UPR; idx += 32) *reinterpret_cast<uint4*>(at(z0 + idx / UPR, idx % UPR)) = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&ready_bar[e]);
                 }
+                if (!mbar_wait_warp(&landed_bar[e], (landed_phase >> e) & 1u, abort_ptr)) { ok = false; return; }
+                landed_phase ^= 1u << e;
+                auto put = [&](int idx, const uint4& x, int page) {
+                    const int pos = first + idx / n_u, u = u0 + idx % n_u;
+                    *reinterpret_cast<uint4*>(at(pos - start, u - u0)) = x;
+                    if (page >= 0 && page < p.a.num_pages)
+                        *reinterpret_cast<uint4*>(pool + (((size_t)page * p.a.Hkv + r.head) * kPageSize + (pos % kPageSize)) * D + u * 8) = x;
+                };
+#pragma unroll
+                for (int k = 0; k < PRE; ++k)
+                    if (k * 32 + lane < n_units) put(k * 32 + lane, val[k], pid[k]);
+                for (int idx = PRE * 32 + lane; idx < n_units; idx += 32) {
+                    const int pos = first + idx / n_u, u = u0 + idx % n_u;
+                    put(idx, *reinterpret_cast<const uint4*>(src + (((size_t)r.seq * R + (pos - r.L)) * p.a.Hkv + r.head) * D + u * 8), pt[pos / kPageSize]);
+                }
+                if (is_v) {
+                    // positions past the end have weight zero, but zero times a stale NaN would still poison P V
+                    const int z0 = max(row0, end - start), n_zero = row0 + n_row - z0;
+                    for (int idx = lane; idx < n_zero * UPR; idx += 32) *reinterpret_cast<uint4*>(at(z0 + idx / UPR, idx % UPR)) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ready_bar[e]);
             }
+        };
+        // K runs ahead of V as the scores do
+        struct Blocks { Run r; int f, t; };
+        Blocks k, v;
+        k.f = f_begin; k.t = 0;
+        bool any = next_run(k.f, k.r);
+        for (; any && !k.r.tail; any = next_run(k.f, k.r)) { ring_at[0] += k.r.n * PARTS; ring_at[1] += k.r.n * PARTS; }      // nothing to patch
+        bool have_v = any;
+        v = k;
+        for (int ahead = 0; have_v && ok;) {
+            if (any && ahead < 2) {
+                patch(k.r, k.t, false);
+                if (++k.t == k.r.n) { any = next_run(k.f, k.r); k.t = 0; }
+                ++ahead;
+                continue;
+            }
+            patch(v.r, v.t, true);
+            if (++v.t == v.r.n) { have_v = next_run(v.f, v.r); v.t = 0; }
+            --ahead;
         }
     } else if (warp == 1) {
         // ------------------------------------------------ products
-        if (lane == 0) {
-            constexpr uint32_t idesc_qk = umma_idesc_bf16(kTileRows, kPrefixBlock, false);
-            constexpr uint32_t idesc_pv = umma_idesc_bf16(kTileRows, D, true);
-            constexpr int kVRegion = kPrefixBlock / PARTS * 128;
-            const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem)), ring = smem_u32(smem);
-            bool ok = true;
-            int it = 0;                              // ring entries taken so far
-            int tau[2] = {0, 0}, runs[2] = {0, 0};   // blocks by score buffer, runs by tile so far
-            auto entry_ready = [&](int i) { if (ok && !mbar_wait(&ready_bar[i % E], ((uint32_t)(i / E)) & 1u, abort_ptr)) ok = false; };
-            // S[buf] = Q_x K^T over `part`'s share of d
-            auto qk = [&](int x, int buf, int i, int part) {
-                tc_fence_after();
-                const uint32_t k_lo = umma_desc_lo(ring + (uint32_t)(i % E) * Cfg::kEntry), d_tmem = tmem_base + (uint32_t)(buf * kPrefixBlock);
+        // The whole warp runs this code, so that addresses and descriptors stay warp-uniform; one elected lane issues.
+        constexpr uint32_t idesc_qk = umma_idesc_bf16(kTileRows, kPrefixBlock, false);
+        constexpr uint32_t idesc_pv = umma_idesc_bf16(kTileRows, D, true);
+        constexpr int kVRegion = kPrefixBlock / PARTS * 128;
+        const uint32_t lead = elect_one();
+        const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem)), k_lo0 = umma_desc_lo(smem_u32(ring_smem));
+        const uint32_t v_lo0 = (((smem_u32(ring_smem) + E * Cfg::kEntry) & 0x3FFFFu) >> 4) | ((uint32_t)(kVRegion >> 4) << 16);
+        bool ok = true;
+        int ek = 0, ev = 0;                                            // ring entries
+        uint32_t lap_k = 0, lap_v = 0, s_lap[2] = {0, 0}, q_lap[2] = {0, 0}, o_lap[2] = {1, 1};       // parities of the next waits
+        auto wait = [&](uint64_t* bar, uint32_t parity) { if (!mbar_wait_warp(bar, parity, abort_ptr)) ok = false; };
+        // S[buf] = Q K^T over `part`'s share of d; the queries q_off bytes into their place
+        auto qk = [&](uint32_t q_off, int buf, int part) {
+            tc_fence_after();
+            const uint32_t k_lo = k_lo0 + (uint32_t)(ek * (Cfg::kEntry >> 4)), a0 = q_lo + (q_off >> 4), d_tmem = tmem_base + (uint32_t)(buf * kPrefixBlock);
 #pragma unroll
-                for (int kk = 0; kk < D / 16 / PARTS; ++kk) {
-                    const int dc = part * (NCH / PARTS) + (kk >> 2);
-                    const uint32_t a = q_lo + (uint32_t)((x * Cfg::kQTile + dc * (kTileRows * 128) + (kk & 3) * 32) >> 4);
-                    const uint32_t bb = k_lo + (uint32_t)(((kk >> 2) * (kPrefixBlock * 128) + (kk & 3) * 32) >> 4);
-                    if (kk == 0 && part == 0) umma_bf16<false>(d_tmem, a, bb, idesc_qk);
-                    else umma_bf16<true>(d_tmem, a, bb, idesc_qk);
-                }
-            };
-            // O_x (+)= P[buf] V over `part`'s share of the positions
-            auto pv = [&](int x, int buf, int i, int part, bool first) {
-                tc_fence_after();
-                const uint32_t v_lo = (((ring + (uint32_t)(i % E) * Cfg::kEntry) & 0x3FFFFu) >> 4) | ((uint32_t)(kVRegion >> 4) << 16);
-                const uint32_t d_tmem = tmem_base + Cfg::kTmemO + (uint32_t)(x * D), a0 = tmem_base + (uint32_t)(buf * kPrefixBlock);
+            for (int kk = 0; kk < D / 16 / PARTS; ++kk) {
+                const int dc = part * (NCH / PARTS) + (kk >> 2);
+                umma_bf16_lead(lead, d_tmem, a0 + (uint32_t)((dc * (kTileRows * 128) + (kk & 3) * 32) >> 4),
+                               k_lo + (uint32_t)(((kk >> 2) * (kPrefixBlock * 128) + (kk & 3) * 32) >> 4), idesc_qk, kk == 0 && part == 0 ? 0u : 1u);
+            }
+        };
+        // O_x (+)= P[buf] V over `part`'s share of the positions
+        auto pv = [&](int x, int buf, int part, bool first) {
+            tc_fence_after();
+            const uint32_t v_lo = v_lo0 + (uint32_t)(ev * (Cfg::kEntry >> 4)), d_tmem = tmem_base + Cfg::kTmemO + (uint32_t)(x * D);
+            const uint32_t a0 = tmem_base + (uint32_t)(buf * kPrefixBlock + part * (kPrefixBlock / PARTS / 2));
 #pragma unroll
-                for (int ks = 0; ks < kPrefixBlock / 16 / PARTS; ++ks) {
-                    const uint32_t a = a0 + (uint32_t)((part * (kPrefixBlock / 16 / PARTS) + ks) * 8), bb = v_lo + (uint32_t)((ks * 2048) >> 4);
-                    if (ks == 0 && part == 0 && first) umma_bf16_ts<false>(d_tmem, a, bb, idesc_pv);
-                    else umma_bf16_ts<true>(d_tmem, a, bb, idesc_pv);
-                }
-            };
-            auto weights_ready = [&](int buf, int count) { if (ok && !mbar_wait(&p_full_bar[buf], (uint32_t)count & 1u, abort_ptr)) ok = false; };
-            auto o_drained = [&](int x) { if (ok && runs[x] > 0 && !mbar_wait(&o_free_bar[x], (uint32_t)(runs[x] - 1) & 1u, abort_ptr)) ok = false; };
-            for (int run = 0; ok && next_run(r); ++run) {
-                const int n = r.n;
-                const bool two = r.n_rows[1] > 0;
-                if (!mbar_wait(&q_ready_bar, (uint32_t)run & 1u, abort_ptr)) { ok = false; break; }
-                if (NT == 2 && !r.tail) {
-                    entry_ready(it);
+            for (int ks = 0; ks < kPrefixBlock / 16 / PARTS; ++ks)
+                umma_bf16_ts_lead(lead, d_tmem, a0 + (uint32_t)(ks * 8), v_lo + (uint32_t)((ks * 2048) >> 4), idesc_pv, ks == 0 && part == 0 && first ? 0u : 1u);
+        };
+        auto k_done = [&]() { umma_commit_lead(lead, &empty_bar[ek]); if (++ek == E) { ek = 0; lap_k ^= 1u; } };
+        auto v_done = [&]() { umma_commit_lead(lead, &empty_bar[E + ev]); if (++ev == E) { ev = 0; lap_v ^= 1u; } };
+        struct Blocks { Run r; int f, t; };
+        Blocks k, v;
+        k.f = f_begin; k.t = 0;
+        bool any = next_run(k.f, k.r);
+        if constexpr (NT == 2) {
+            for (; ok && any && paired(k.r); any = next_run(k.f, k.r)) {
+                const int n = k.r.n;
+                const bool two = k.r.n_rows[1] > 0;
+                wait(&q_ready_bar[0], q_lap[0]); q_lap[0] ^= 1u;
+                for (int t = -1; t < n && ok; ++t) {
+                    // the weights of block t times V, then, over each tile's P, the scores of block t + 1
+                    if (t >= 0) wait(&ready_bar[E + ev], lap_v);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (x == 1 && !two) break;
+                        if (t >= 0) {
+                            wait(&p_full_bar[x], s_lap[x]); s_lap[x] ^= 1u;
+                            if (t == 0) { wait(&o_free_bar[x], o_lap[x]); o_lap[x] ^= 1u; }
+                            if (!ok) break;
+                            pv(x, x, 0, t == 0);
+                        }
+                        if (t + 1 < n) {
+                            if (x == 0) { wait(&ready_bar[ek], lap_k); if (!ok) break; }
+                            qk((uint32_t)(x * Cfg::kQTile), x, 0);
+                            umma_commit_lead(lead, &s_full_bar[x]);
+                        } else {
+                            umma_commit_lead(lead, &o_full_bar[x]);
+                        }
+                    }
                     if (!ok) break;
-                    qk(0, 0, it, 0); umma_commit(&s_full_bar[0]);
-                    if (two) { qk(1, 1, it, 0); umma_commit(&s_full_bar[1]); }
-                    umma_commit(&empty_bar[it % E]);
-                    if (n == 1) umma_commit(&q_free_bar);
-                    ++it;
-                    for (int t = 0; t < n && ok; ++t) {
-                        const int iv = it, ik = it + 1;               // V of this block, K of the next
-                        const bool more = t + 1 < n;
-                        it += more ? 2 : 1;
-                        entry_ready(iv);
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            if (x == 1 && !two) break;
-                            weights_ready(x, tau[x] + t);
-                            if (t == 0) o_drained(x);
-                            if (!ok) break;
-                            pv(x, x, iv, 0, t == 0);
-                            if (x == (two ? 1 : 0)) umma_commit(&empty_bar[iv % E]);
-                            if (more) {
-                                if (x == 0) { entry_ready(ik); if (!ok) break; }
-                                qk(x, x, ik, 0);                       // over this tile's P, behind the product that read it
-                                umma_commit(&s_full_bar[x]);
-                            } else {
-                                umma_commit(&o_full_bar[x]);
-                            }
-                        }
-                        if (ok && more) {
-                            umma_commit(&empty_bar[ik % E]);
-                            if (t + 2 == n) umma_commit(&q_free_bar);
-                        }
-                    }
-                    tau[0] += n; runs[0] += 1;
-                    if (two) { tau[1] += n; runs[1] += 1; }
-                } else {
-                    // Scores ahead of the weights: block t's buffer takes the scores of block t + 2 behind the product that read its P.  One
-                    // accumulator (head_dim 256), or even and odd blocks with one each, by buffer; buffers alternate from run to run where there is
-                    // one accumulator, and start at 0 where there are two.
-                    const int b0 = NT == 1 ? tau[0] & 1 : 0;
-                    int done[2] = {0, 0};                              // blocks of this run by score buffer (two accumulators)
-                    auto scores = [&](int t) {
-                        const int buf = (b0 + t) & 1;
-#pragma unroll
-                        for (int part = 0; part < PARTS; ++part, ++it) {
-                            entry_ready(it);
-                            if (!ok) return;
-                            qk(0, buf, it, part);
-                            umma_commit(&empty_bar[it % E]);
-                        }
-                        umma_commit(&s_full_bar[buf]);
-                        if (t == n - 1) umma_commit(&q_free_bar);
-                    };
-                    scores(0);
-                    if (ok && n > 1) scores(1);
-                    for (int t = 0; t < n && ok; ++t) {
-                        const int buf = (b0 + t) & 1, x = NT == 1 ? 0 : buf;
-                        weights_ready(buf, NT == 1 ? (tau[0] + t) >> 1 : tau[buf] + done[buf]);
-                        if (NT == 1 ? t == 0 : t < 2) o_drained(x);
-#pragma unroll
-                        for (int part = 0; part < PARTS; ++part, ++it) {
-                            entry_ready(it);
-                            if (!ok) break;
-                            pv(x, buf, it, part, NT == 1 ? t == 0 : t < 2);
-                            umma_commit(&empty_bar[it % E]);
-                        }
-                        if (!ok) break;
-                        ++done[buf];
-                        if (NT == 1) umma_commit(&pv_done_bar);
-                        if (NT == 1 ? t == n - 1 : t >= n - 2) umma_commit(&o_full_bar[x]);
-                        if (t + 2 < n) scores(t + 2);
-                    }
-                    if (NT == 1) { tau[0] += n; runs[0] += 1; }
-                    else { tau[0] += done[0]; tau[1] += done[1]; runs[0] += 1; if (n > 1) runs[1] += 1; }
+                    if (t >= 0) v_done();
+                    if (t + 1 < n) k_done();
+                    if (t + 2 == n) umma_commit_lead(lead, &q_free_bar[0]);
                 }
             }
+        }
+        // The pipeline: a block's scores go over the P of two blocks before, behind the product that read it.
+        bool have_v = any && ok;
+        v = k;
+        int turn = 0, n_s = 0, n_p = 0;                               // tails so far (scores), blocks so far
+        while (have_v && ok) {
+            if (any && n_s < n_p + 2) {
+                const int qb = k.r.tail ? turn & 1 : 0, buf = n_s++ & 1;
+                if (k.t == 0) { wait(&q_ready_bar[qb], qb ? q_lap[1] : q_lap[0]); if (qb) q_lap[1] ^= 1u; else q_lap[0] ^= 1u; }
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                    wait(&ready_bar[ek], lap_k);
+                    if (!ok) break;
+                    qk((uint32_t)(qb * kQTurn), buf, part);
+                    k_done();
+                }
+                if (!ok) break;
+                umma_commit_lead(lead, &s_full_bar[buf]);
+                if (++k.t == k.r.n) {
+                    umma_commit_lead(lead, &q_free_bar[qb]);
+                    if (k.r.tail) ++turn;
+                    any = next_run(k.f, k.r);
+                    k.t = 0;
+                }
+                continue;
+            }
+            const int buf = n_p++ & 1, x = NT == 2 ? buf : 0, n = v.r.n;
+            const bool first = NT == 2 ? v.t < 2 : v.t == 0, last = NT == 2 ? v.t >= n - 2 : v.t == n - 1;      // of this accumulator
+            wait(&p_full_bar[buf], buf ? s_lap[1] : s_lap[0]); if (buf) s_lap[1] ^= 1u; else s_lap[0] ^= 1u;
+            if (first) { wait(&o_free_bar[x], x ? o_lap[1] : o_lap[0]); if (x) o_lap[1] ^= 1u; else o_lap[0] ^= 1u; }
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+                wait(&ready_bar[E + ev], lap_v);
+                if (!ok) break;
+                pv(x, buf, part, first);
+                v_done();
+            }
+            if (!ok) break;
+            if (NT == 1) umma_commit_lead(lead, &pv_done_bar);
+            if (last) umma_commit_lead(lead, &o_full_bar[x]);
+            if (++v.t == n) { have_v = next_run(v.f, v.r); v.t = 0; }
         }
     } else if (warp >= 4) {
         // ------------------------------------------------ softmax: a row per thread
@@ -579,14 +594,18 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const uint32_t tmem_o = tmem_base + Cfg::kTmemO + (uint32_t)(x * D) + lane_base;
         const float scale_log2 = p.a.scale * 1.4426950408889634f;
         bool ok = true;
-        int tau = 0, runs = 0;
-        while (ok && next_run(r)) {
-            if (r.n_rows[x] == 0) continue;
-            const bool alone = r.tail && NT == 2;                      // every second block is this tile's
+        int tau = 0, uses = 0, f = f_begin;
+        int at = 0;                                                    // blocks of the pipeline ahead of this run
+        Run r;
+        while (ok && next_run(f, r)) {
+            const bool alone = r.tail && NT == 2;                      // every second block is this accumulator's
+            const int turn = alone ? (at & 1) ^ x : x;                 // its first block; the place of its piece
+            if (alone) at += r.n;
+            if (alone ? turn >= r.n : r.n_rows[x] == 0) continue;
             const bool some = (warp & 3) * 32 < r.n_rows[x];           // this warp has rows
             const int j = min(row / G, R - 1);                         // tail: block row
             float ref = -INFINITY, l_run = 0.f;
-            for (int t = alone ? x : 0; t < r.n && ok; t += alone ? 2 : 1, ++tau) {
+            for (int t = alone ? turn : 0; t < r.n && ok; t += alone ? 2 : 1, ++tau) {
                 const int buf = NT == 2 ? x : tau & 1;
                 const uint32_t parity = (uint32_t)(NT == 2 ? tau : tau >> 1) & 1u;
                 if (!mbar_wait_warp(&s_full_bar[buf], parity, abort_ptr)) { ok = false; break; }
@@ -648,12 +667,12 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_full_bar[buf]);
             }
-            if (!ok || !mbar_wait_warp(&o_full_bar[x], (uint32_t)runs & 1u, abort_ptr)) { ok = false; break; }
-            ++runs;
+            if (!ok || !mbar_wait_warp(&o_full_bar[x], (uint32_t)uses & 1u, abort_ptr)) { ok = false; break; }
+            ++uses;
             tc_fence_after();
             if (some) {
                 // ---- the piece
-                const Piece pc = piece_at(p, r.slot, x, D);
+                const Piece pc = piece_at(p, r.slot, turn, D);
                 const bool live = row < r.n_rows[x];
 #pragma unroll 1
                 for (int c0 = 0; c0 < D; c0 += 32) {
@@ -696,22 +715,19 @@ __global__ void __launch_bounds__(kMergeThreads) attn_shared_merge_kernel(const 
     pdl_trigger();
     const int4 seq = p.seqs[b], grp = p.seq_groups[b];
     const int per = p.meta[0], tails0 = p.meta[1];
-    if (seq.y == 0 || c8 * 8 >= D) return;                             // skipped; past the last unit
+    if (seq.y <= 0 || c8 * 8 >= D) return;                             // skipped; past the last unit
     // An item's pieces: consecutive CTAs of the kernel above; alone in one, it has a slot of its own.
-    struct Pieces { int start, blocks, cost, c0, c1, item; };
-    auto pieces_of = [&](int start, int blocks, int cost, int item) {
-        return Pieces{start, blocks, cost, start / per, (start + (blocks - 1) * cost) / per, item};
-    };
+    struct Pieces { int start, c0, c1, item; };
+    auto pieces_of = [&](int start, int blocks, int cost, int extra, int item) { return Pieces{start, start / per, block_begin(blocks - 1, start, cost, extra) / per, item}; };
     auto slot_of = [&](const Pieces& q, int c) { return q.c0 == q.c1 ? -1 - q.item : c * 2 + (q.start < c * per ? 0 : 1); };
-    const Pieces tl = pieces_of(tails0 + (seq.x * p.a.Hkv + h * seq.y) * kCostTail, seq.y, kCostTail, p.slots.prefix_items + b * p.a.Hkv + h);
+    const Pieces tl = pieces_of(tails0 + seq.x * p.a.Hkv + h * (seq.y * kCostTail + kCostTailItem), seq.y, kCostTail, kCostTailItem, p.slots.prefix_items + b * p.a.Hkv + h);
     const int pair = seq.z + row / G, tile = pair / nb, k = tile / tiles_per_item * p.a.Hkv + h;
     const int prow = (pair - tile * nb) * G + row % G, px = tile % tiles_per_item;
-    Pieces pf{0, 0, 1, 0, -1, 0};
-    if (seq.w > 0) pf = pieces_of(grp.x + k * seq.w * grp.z, seq.w, grp.z, grp.y + k);
+    Pieces pf{0, 0, -1, 0};
+    if (seq.w > 0) pf = pieces_of(grp.x + k * (seq.w * grp.z + kCostPrefixItem), seq.w, grp.z, kCostPrefixItem, grp.y + k);
     // a tail's piece is in two accumulators where it has more than one block
     auto tail_tiles = [&](int c) {
-        const long long lo = max(0LL, (long long)c * per - tl.start), hi = (long long)(c + 1) * per - tl.start;
-        const int k0 = (int)((lo + kCostTail - 1) / kCostTail), k1 = (int)min((long long)tl.blocks, (hi + kCostTail - 1) / kCostTail);
+        const int k0 = first_block(c * per, tl.start, kCostTail, kCostTailItem), k1 = min(seq.y, first_block((c + 1) * per, tl.start, kCostTail, kCostTailItem));
         return min(tiles_per_item, k1 - k0);
     };
     float m = -INFINITY;
@@ -748,17 +764,18 @@ template <int D>
 cudaError_t launch(const SharedAttnParams& p, cudaStream_t stream) {
     using Cfg = SharedCfg<D>;
     const int G = p.a.Hq / p.a.Hkv;
-    CUtensorMap mk, mv, mq;
+    CUtensorMap mk, mv, mq, mqt;
     const uint64_t rows_total = (uint64_t)p.a.num_pages * p.a.Hkv * kPageSize;
     if (!make_tensor_map_bf16_2d(&mk, p.a.k_pages, rows_total, D, kPageSize) || !make_tensor_map_bf16_2d(&mv, p.a.v_pages, rows_total, D, kPageSize) ||
-        !make_tensor_map_bf16_heads(&mq, p.a.q, (uint64_t)p.a.B * p.a.R, (uint64_t)p.a.Hq, D, (uint32_t)(kTileRows / G), (uint32_t)G))
+        !make_tensor_map_bf16_heads(&mq, p.a.q, (uint64_t)p.a.B * p.a.R, (uint64_t)p.a.Hq, D, (uint32_t)(kTileRows / G), (uint32_t)G) ||
+        !make_tensor_map_bf16_heads(&mqt, p.a.q, (uint64_t)p.a.B * p.a.R, (uint64_t)p.a.Hq, D, (uint32_t)p.a.R, (uint32_t)G))
         return cudaErrorInvalidValue;
     cudaError_t e = cudaFuncSetAttribute(attn_shared_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kMaxSmem);
     if (e != cudaSuccess) return e;
     int ctas = device_sm_count();
     if (ctas > kSharedMaxCtas) ctas = kSharedMaxCtas;
     const size_t smem = Cfg::kSmem + (size_t)(p.a.B + 1 + 5 * (p.n_groups + 1)) * 4;
-    e = launch_pdl(attn_shared_kernel<D>, dim3(ctas), dim3(Cfg::kThreads), smem, stream, mk, mv, mq, p);
+    e = launch_pdl(attn_shared_kernel<D>, dim3(ctas), dim3(Cfg::kThreads), smem, stream, mk, mv, mq, mqt, p);
     if (e != cudaSuccess) return e;
     const int units = G * p.a.R * (D / 8);
     return launch_pdl(attn_shared_merge_kernel, dim3(p.a.B * p.a.Hkv, (units + kMergeThreads - 1) / kMergeThreads), dim3(kMergeThreads), 0, stream, p, Cfg::kTiles);

@@ -81,6 +81,7 @@ __device__ __forceinline__ void tmem_ld_row32(uint32_t taddr, uint32_t* r) {
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr));
 }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 template <int N>
 __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[N]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -144,15 +145,17 @@ __device__ __forceinline__ int find_last(const int* cum, int n, int u) {       /
 
 // A run of blocks of one item.
 struct Run {
-    bool tail;
+    int tail;            // (truth value)
     int head, seq;       // seq: whose page table is read
     int blk0;            // first (sequence, block row) pair of the rows
     int n_rows[2];       // query rows of each tile
     int pos0;            // position of the first block
-    int n;               // blocks
+    int n;               // blocks; 0 behind the last run
     int L;               // tail: committed length
     int slot;            // slot of its piece: >= 0 one of the CTA's two, else -1 - item for an item that the CTA has all of (prefix items, then tails)
 };
+
+constexpr int kRunQueue = 8;
 
 template <int D>
 __global__ void __launch_bounds__(SharedCfg<D>::kThreads, 1)
@@ -166,9 +169,11 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __shared__ __align__(8) uint64_t ready_bar[2 * E], empty_bar[2 * E];
     __shared__ __align__(8) uint64_t landed_bar[2 * E];                // the bytes of an entry that still needs patching
     __shared__ __align__(8) uint64_t q_ready_bar[2], q_free_bar[2];   // by query buffer: a prefix item has both, tails take turns
-    __shared__ __align__(8) uint64_t s_full_bar[2], p_full_bar[2];     // by score buffer
+    __shared__ __align__(8) uint64_t s_full_bar[2], p_full_bar[2][2];  // by score buffer; weights of the first and the second 64 positions
     __shared__ __align__(8) uint64_t o_full_bar[2], o_free_bar[2];     // by tile
     __shared__ __align__(8) uint64_t pv_done_bar;                      // one tile: O is up to date
+    __shared__ __align__(8) uint64_t run_ready_bar[kRunQueue], run_free_bar[kRunQueue];      // the runs, worked out by the K warp for all
+    __shared__ Run s_runs[kRunQueue];
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag, s_bad;
 
@@ -178,7 +183,8 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (threadIdx.x == 0) {
         for (int e = 0; e < 2 * E; ++e) { mbar_init(&ready_bar[e], 1); mbar_init(&empty_bar[e], 1); mbar_init(&landed_bar[e], 1); }
         mbar_init(&pv_done_bar, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&q_ready_bar[i], 1); mbar_init(&q_free_bar[i], 1); mbar_init(&s_full_bar[i], 1); mbar_init(&p_full_bar[i], 4); mbar_init(&o_full_bar[i], 1); mbar_init(&o_free_bar[i], 4); }
+        for (int i = 0; i < kRunQueue; ++i) { mbar_init(&run_ready_bar[i], 1); mbar_init(&run_free_bar[i], 3 + 4 * NT); }      // V, helper, products, softmax
+        for (int i = 0; i < 2; ++i) { mbar_init(&q_ready_bar[i], 1); mbar_init(&q_free_bar[i], 1); mbar_init(&s_full_bar[i], 1); mbar_init(&p_full_bar[i][0], 4); mbar_init(&p_full_bar[i][1], 4); mbar_init(&o_full_bar[i], 1); mbar_init(&o_free_bar[i], 4); }
         abort_flag = 0;
         s_bad = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -295,7 +301,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 const int length = n_all * cost + extra, k = (f - ln.gcost[g]) / length, tile = k / p.a.Hkv, done = tile * nb * NT;
                 start = ln.gcost[g] + k * length;
                 item = ln.gitem[g] + k;
-                r.tail = false;
+                r.tail = 0;
                 r.head = k - tile * p.a.Hkv;
                 r.seq = ln.gsrc[g];
                 r.blk0 = ln.gs[g] * R + done;
@@ -311,7 +317,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 r.head = (u - ln.tail[b] * p.a.Hkv) / length;
                 start = tails0 + ln.tail[b] * p.a.Hkv + r.head * length;
                 item = p.slots.prefix_items + b * p.a.Hkv + r.head;
-                r.tail = true;
+                r.tail = 1;
                 r.seq = b;
                 r.blk0 = b * R;
                 r.n_rows[0] = r.n_rows[1] = R * G;
@@ -327,6 +333,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             r.slot = k0 == 0 && k1 == n_all ? -1 - item : (int)blockIdx.x * 2 + (k0 > 0 ? 0 : 1);
             return true;
         }
+        r.n = 0;
         return false;
     };
     // Two tiles on one prefix; everything else is one pipeline over all blocks, in which the scores run two blocks ahead.
@@ -334,6 +341,15 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
     constexpr uint32_t tmem_base = 0;                                  // all 512 columns are this CTA's: they begin at 0
     volatile int* abort_ptr = &abort_flag;
+    // Run i of the queue; n 0 where there is none (or a wait gave up).  keep: the caller reads it again.
+    auto take_run = [&](int i, Run& r, bool keep) -> bool {
+        const bool ok = mbar_wait_warp(&run_ready_bar[i % kRunQueue], (uint32_t)(i / kRunQueue) & 1u, abort_ptr);
+        r = s_runs[i % kRunQueue];
+        if (!ok) r.n = 0;
+        __syncwarp();
+        if (!keep && lane == 0) mbar_arrive(&run_free_bar[i % kRunQueue]);
+        return r.n > 0;
+    };
     if (warp == 0 || warp == 3) {
         // ------------------------------------------------ copies: K (and the queries) by warp 0, V by warp 3
         const bool is_v = warp == 3;
@@ -350,7 +366,19 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         int q_uses[2] = {0, 0};
         bool ok = true;
         Run r;
-        while (ok && next_run(f, r)) {
+        for (int run = 0; ok; ++run) {
+            if (is_v) {
+                if (!take_run(run, r, false)) break;
+            } else {
+                if (run >= kRunQueue && !mbar_wait_warp(&run_free_bar[run % kRunQueue], (uint32_t)(run / kRunQueue - 1) & 1u, abort_ptr)) break;
+                const bool any = next_run(f, r);
+                if (lane == 0) {
+                    s_runs[run % kRunQueue] = r;
+                    mbar_arrive(&run_ready_bar[run % kRunQueue]);
+                }
+                __syncwarp();
+                if (!any) break;
+            }
             if (!is_v) {
                 const int buf = r.tail ? turn++ & 1 : 0, used = buf ? q_uses[1]++ : q_uses[0]++;
                 if (used > 0 && !mbar_wait_warp(&q_free_bar[buf], (uint32_t)(used - 1) & 1u, abort_ptr)) break;
@@ -457,23 +485,23 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
         };
         // K runs ahead of V as the scores do
-        struct Blocks { Run r; int f, t; };
+        struct Blocks { Run r; int run, t; };
         Blocks k, v;
-        k.f = f_begin; k.t = 0;
-        bool any = next_run(k.f, k.r);
-        for (; any && !k.r.tail; any = next_run(k.f, k.r)) { ring_at[0] += k.r.n * PARTS; ring_at[1] += k.r.n * PARTS; }      // nothing to patch
-        bool have_v = any;
+        k.run = 0; k.t = 0;
+        bool any = take_run(0, k.r, true);
         v = k;
+        bool have_v = any;
         for (int ahead = 0; have_v && ok;) {
-            if (any && ahead < 2) {
-                patch(k.r, k.t, false);
-                if (++k.t == k.r.n) { any = next_run(k.f, k.r); k.t = 0; }
-                ++ahead;
-                continue;
+            const bool is_v = !(any && ahead < 2);
+            Blocks& w = is_v ? v : k;
+            patch(w.r, w.t, is_v);
+            if (++w.t == w.r.n) {
+                if (is_v && lane == 0) mbar_arrive(&run_free_bar[v.run % kRunQueue]);
+                w.t = 0;
+                const bool more = take_run(++w.run, w.r, true);
+                if (is_v) have_v = more; else any = more;
             }
-            patch(v.r, v.t, true);
-            if (++v.t == v.r.n) { have_v = next_run(v.f, v.r); v.t = 0; }
-            --ahead;
+            ahead += is_v ? -1 : 1;
         }
     } else if (warp == 1) {
         // ------------------------------------------------ products
@@ -499,25 +527,27 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                                k_lo + (uint32_t)(((kk >> 2) * (kPrefixBlock * 128) + (kk & 3) * 32) >> 4), idesc_qk, kk == 0 && part == 0 ? 0u : 1u);
             }
         };
-        // O_x (+)= P[buf] V over `part`'s share of the positions
-        auto pv = [&](int x, int buf, int part, bool first) {
+        // O_x (+)= P[buf] V over one half of the positions
+        auto pv = [&](int x, int buf, int half, bool first) {
             tc_fence_after();
-            const uint32_t v_lo = v_lo0 + (uint32_t)(ev * (Cfg::kEntry >> 4)), d_tmem = tmem_base + Cfg::kTmemO + (uint32_t)(x * D);
-            const uint32_t a0 = tmem_base + (uint32_t)(buf * kPrefixBlock + part * (kPrefixBlock / PARTS / 2));
+            const uint32_t v_lo = v_lo0 + (uint32_t)(ev * (Cfg::kEntry >> 4) + (PARTS == 1 ? half * (kPrefixBlock / 2 * 128 >> 4) : 0));
+            const uint32_t d_tmem = tmem_base + Cfg::kTmemO + (uint32_t)(x * D), a0 = tmem_base + (uint32_t)(buf * kPrefixBlock + half * (kPrefixBlock / 4));
 #pragma unroll
-            for (int ks = 0; ks < kPrefixBlock / 16 / PARTS; ++ks)
-                umma_bf16_ts_lead(lead, d_tmem, a0 + (uint32_t)(ks * 8), v_lo + (uint32_t)((ks * 2048) >> 4), idesc_pv, ks == 0 && part == 0 && first ? 0u : 1u);
+            for (int ks = 0; ks < kPrefixBlock / 32; ++ks)
+                umma_bf16_ts_lead(lead, d_tmem, a0 + (uint32_t)(ks * 8), v_lo + (uint32_t)((ks * 2048) >> 4), idesc_pv, ks == 0 && first ? 0u : 1u);
         };
         auto k_done = [&]() { umma_commit_lead(lead, &empty_bar[ek]); if (++ek == E) { ek = 0; lap_k ^= 1u; } };
         auto v_done = [&]() { umma_commit_lead(lead, &empty_bar[E + ev]); if (++ev == E) { ev = 0; lap_v ^= 1u; } };
-        struct Blocks { Run r; int f, t; };
-        Blocks k, v;
-        k.f = f_begin; k.t = 0;
-        bool any = next_run(k.f, k.r);
+        // (blocks of the scores and of the products: run, block within, blocks of the run)
+        Run kr, vr;
+        int k_run = 0, k_t = 0, v_run, v_t = 0;
+        bool any = take_run(0, kr, true);
         if constexpr (NT == 2) {
-            for (; ok && any && paired(k.r); any = next_run(k.f, k.r)) {
-                const int n = k.r.n;
-                const bool two = k.r.n_rows[1] > 0;
+            for (; ok && any && paired(kr); any = take_run(k_run, kr, true)) {
+                if (lane == 0) mbar_arrive(&run_free_bar[k_run % kRunQueue]);
+                ++k_run;
+                const int n = kr.n;
+                const bool two = kr.n_rows[1] > 0;
                 wait(&q_ready_bar[0], q_lap[0]); q_lap[0] ^= 1u;
                 for (int t = -1; t < n && ok; ++t) {
                     // the weights of block t times V, then, over each tile's P, the scores of block t + 1
@@ -526,10 +556,13 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     for (int x = 0; x < 2; ++x) {
                         if (x == 1 && !two) break;
                         if (t >= 0) {
-                            wait(&p_full_bar[x], s_lap[x]); s_lap[x] ^= 1u;
                             if (t == 0) { wait(&o_free_bar[x], o_lap[x]); o_lap[x] ^= 1u; }
+                            wait(&p_full_bar[x][0], s_lap[x]);
                             if (!ok) break;
                             pv(x, x, 0, t == 0);
+                            wait(&p_full_bar[x][1], s_lap[x]); s_lap[x] ^= 1u;
+                            if (!ok) break;
+                            pv(x, x, 1, false);
                         }
                         if (t + 1 < n) {
                             if (x == 0) { wait(&ready_bar[ek], lap_k); if (!ok) break; }
@@ -547,13 +580,14 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             }
         }
         // The pipeline: a block's scores go over the P of two blocks before, behind the product that read it.
+        vr = kr;
+        v_run = k_run;
         bool have_v = any && ok;
-        v = k;
         int turn = 0, n_s = 0, n_p = 0;                               // tails so far (scores), blocks so far
         while (have_v && ok) {
             if (any && n_s < n_p + 2) {
-                const int qb = k.r.tail ? turn & 1 : 0, buf = n_s++ & 1;
-                if (k.t == 0) { wait(&q_ready_bar[qb], qb ? q_lap[1] : q_lap[0]); if (qb) q_lap[1] ^= 1u; else q_lap[0] ^= 1u; }
+                const int qb = kr.tail ? turn & 1 : 0, buf = n_s++ & 1;
+                if (k_t == 0) { wait(&q_ready_bar[qb], qb ? q_lap[1] : q_lap[0]); if (qb) q_lap[1] ^= 1u; else q_lap[0] ^= 1u; }
 #pragma unroll
                 for (int part = 0; part < PARTS; ++part) {
                     wait(&ready_bar[ek], lap_k);
@@ -563,29 +597,35 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 }
                 if (!ok) break;
                 umma_commit_lead(lead, &s_full_bar[buf]);
-                if (++k.t == k.r.n) {
+                if (++k_t == kr.n) {
                     umma_commit_lead(lead, &q_free_bar[qb]);
-                    if (k.r.tail) ++turn;
-                    any = next_run(k.f, k.r);
-                    k.t = 0;
+                    if (kr.tail) ++turn;
+                    any = take_run(++k_run, kr, true);
+                    k_t = 0;
                 }
                 continue;
             }
-            const int buf = n_p++ & 1, x = NT == 2 ? buf : 0, n = v.r.n;
-            const bool first = NT == 2 ? v.t < 2 : v.t == 0, last = NT == 2 ? v.t >= n - 2 : v.t == n - 1;      // of this accumulator
-            wait(&p_full_bar[buf], buf ? s_lap[1] : s_lap[0]); if (buf) s_lap[1] ^= 1u; else s_lap[0] ^= 1u;
+            const int buf = n_p++ & 1, x = NT == 2 ? buf : 0;
+            const bool first = NT == 2 ? v_t < 2 : v_t == 0, last = NT == 2 ? v_t >= vr.n - 2 : v_t == vr.n - 1;      // of this accumulator
+            const uint32_t lap = buf ? s_lap[1] : s_lap[0];
+            if (buf) s_lap[1] ^= 1u; else s_lap[0] ^= 1u;
             if (first) { wait(&o_free_bar[x], x ? o_lap[1] : o_lap[0]); if (x) o_lap[1] ^= 1u; else o_lap[0] ^= 1u; }
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-                wait(&ready_bar[E + ev], lap_v);
+            for (int half = 0; half < 2; ++half) {
+                if (half == 0 || PARTS == 2) wait(&ready_bar[E + ev], lap_v);
+                wait(&p_full_bar[buf][half], lap);
                 if (!ok) break;
-                pv(x, buf, part, first);
-                v_done();
+                pv(x, buf, half, first && half == 0);
+                if (half == 1 || PARTS == 2) v_done();
             }
             if (!ok) break;
             if (NT == 1) umma_commit_lead(lead, &pv_done_bar);
             if (last) umma_commit_lead(lead, &o_full_bar[x]);
-            if (++v.t == n) { have_v = next_run(v.f, v.r); v.t = 0; }
+            if (++v_t == vr.n) {
+                if (lane == 0) mbar_arrive(&run_free_bar[v_run % kRunQueue]);
+                have_v = take_run(++v_run, vr, true);
+                v_t = 0;
+            }
         }
     } else if (warp >= 4) {
         // ------------------------------------------------ softmax: a row per thread
@@ -594,10 +634,10 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const uint32_t tmem_o = tmem_base + Cfg::kTmemO + (uint32_t)(x * D) + lane_base;
         const float scale_log2 = p.a.scale * 1.4426950408889634f;
         bool ok = true;
-        int tau = 0, uses = 0, f = f_begin;
+        int tau = 0, uses = 0;
         int at = 0;                                                    // blocks of the pipeline ahead of this run
         Run r;
-        while (ok && next_run(f, r)) {
+        for (int run = 0; ok && take_run(run, r, false); ++run) {
             const bool alone = r.tail && NT == 2;                      // every second block is this accumulator's
             const int turn = alone ? (at & 1) ^ x : x;                 // its first block; the place of its piece
             if (alone) at += r.n;
@@ -612,19 +652,25 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 tc_fence_after();
                 if (some) {
                     const uint32_t tmem_s = tmem_base + lane_base + (uint32_t)(buf * kPrefixBlock);
-                    uint32_t s[kPrefixBlock];
-#pragma unroll
-                    for (int c = 0; c < kPrefixBlock; c += 32) tmem_ld_row32(tmem_s + (uint32_t)c, s + c);
-                    tmem_ld_wait(s);
+                    // (Two passes over the scores in tensor memory, 64 columns at a time: holding a row's 128 in registers makes straight-line
+                    // code of 20 KB, which the first blocks of a CTA wait for instruction by instruction.)
                     const int start = r.pos0 + t * kPrefixBlock;
-                    if (r.tail && start + kPrefixBlock > r.L + 1) {    // a position ahead of some row, or past the end
-                        const int seen = r.L + j - start;              // the last column this row sees
-#pragma unroll
-                        for (int c = 0; c < kPrefixBlock; ++c) s[c] = c > seen ? 0xff800000u : s[c];
-                    }
+                    const int seen = r.tail && start + kPrefixBlock > r.L + 1 ? r.L + j - start : kPrefixBlock;      // the last column this row sees
+                    const bool masked = seen < kPrefixBlock;
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kPrefixBlock; c0 += 64) {
+                        uint32_t s[64];
+                        tmem_ld_row32(tmem_s + (uint32_t)c0, s);
+                        tmem_ld_row32(tmem_s + (uint32_t)(c0 + 32), s + 32);
+                        tmem_ld_wait(s);
+                        if (masked) {
 #pragma unroll
-                    for (int c = 0; c < kPrefixBlock; c += 2) m4[(c >> 1) & 3] = fmaxf(m4[(c >> 1) & 3], fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
+                            for (int c = 0; c < 64; ++c) s[c] = c0 + c > seen ? 0xff800000u : s[c];
+                        }
+#pragma unroll
+                        for (int c = 0; c < 64; c += 2) m4[(c >> 1) & 3] = max3(m4[(c >> 1) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                    }
                     const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale_log2;        // (the scale is positive)
                     // The reference moves when the row's maximum has outgrown it by the threshold; O and l follow it.
                     float factor = 1.f;
@@ -647,25 +693,38 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                         l_run *= factor;
                     }
                     const float neg = ref == -INFINITY ? 0.f : -ref;
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+                    const uint64_t scale2 = pack2(scale_log2, scale_log2), neg2 = pack2(neg, neg);
+                    uint64_t part[4] = {0, 0, 0, 0};                   // sums of pairs
+#pragma unroll 1
                     for (int h = 0; h < 2; ++h) {
-                        uint32_t pk[32];
+                        uint32_t s[64], pk[32];
+                        tmem_ld_row32(tmem_s + (uint32_t)(h * 64), s);
+                        tmem_ld_row32(tmem_s + (uint32_t)(h * 64 + 32), s + 32);
+                        tmem_ld_wait(s);
+                        if (masked) {
+#pragma unroll
+                            for (int c = 0; c < 64; ++c) s[c] = h * 64 + c > seen ? 0xff800000u : s[c];
+                        }
 #pragma unroll
                         for (int c = 0; c < 32; ++c) {
-                            const float p0 = ex2_ftz(fmaf(__uint_as_float(s[h * 64 + 2 * c]), scale_log2, neg));
-                            const float p1 = ex2_ftz(fmaf(__uint_as_float(s[h * 64 + 2 * c + 1]), scale_log2, neg));
-                            part[c & 3] += p0 + p1;
+                            const float2 e = unpack2(fma2(pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), scale2, neg2));
+                            const float p0 = ex2_ftz(e.x), p1 = ex2_ftz(e.y);
+                            part[c & 3] = add2(part[c & 3], pack2(p0, p1));
                             pk[c] = bf16x2(p0, p1);
                         }
+                        // (over columns that have been read: P is half as wide as S)
                         tmem_st_row32(tmem_s + (uint32_t)(h * 32), pk);
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&p_full_bar[buf][h]);
                     }
-                    l_run += (part[0] + part[1]) + (part[2] + part[3]);
-                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    const float2 sum = unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])));
+                    l_run += sum.x + sum.y;
+                } else {
+                    tc_fence_before();
+                    if (lane == 0) { mbar_arrive(&p_full_bar[buf][0]); mbar_arrive(&p_full_bar[buf][1]); }
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full_bar[buf]);
             }
             if (!ok || !mbar_wait_warp(&o_full_bar[x], (uint32_t)uses & 1u, abort_ptr)) { ok = false; break; }
             ++uses;

@@ -172,6 +172,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __shared__ __align__(8) uint64_t s_full_bar[2], p_full_bar[2][2];  // by score buffer; weights of the first and the second 64 positions
     __shared__ __align__(8) uint64_t o_full_bar[2], o_free_bar[2];     // by tile
     __shared__ __align__(8) uint64_t pv_done_bar;                      // one tile: O is up to date
+    __shared__ __align__(8) uint64_t pv_half_bar[2];                   // by accumulator: it has the first 64 positions of a block
     __shared__ __align__(8) uint64_t run_ready_bar[kRunQueue], run_free_bar[kRunQueue];      // the runs, worked out by the K warp for all
     __shared__ Run s_runs[kRunQueue];
     __shared__ uint32_t tmem_base_slot;
@@ -182,7 +183,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     const int G = p.a.Hq / p.a.Hkv, nb = kTileRows / G, tile_rows = nb * G;
     if (threadIdx.x == 0) {
         for (int e = 0; e < 2 * E; ++e) { mbar_init(&ready_bar[e], 1); mbar_init(&empty_bar[e], 1); mbar_init(&landed_bar[e], 1); }
-        mbar_init(&pv_done_bar, 1);
+        mbar_init(&pv_done_bar, 1); mbar_init(&pv_half_bar[0], 1); mbar_init(&pv_half_bar[1], 1);
         for (int i = 0; i < kRunQueue; ++i) { mbar_init(&run_ready_bar[i], 1); mbar_init(&run_free_bar[i], 3 + 4 * NT); }      // V, helper, products, softmax
         for (int i = 0; i < 2; ++i) { mbar_init(&q_ready_bar[i], 1); mbar_init(&q_free_bar[i], 1); mbar_init(&s_full_bar[i], 1); mbar_init(&p_full_bar[i][0], 4); mbar_init(&p_full_bar[i][1], 4); mbar_init(&o_full_bar[i], 1); mbar_init(&o_free_bar[i], 4); }
         abort_flag = 0;
@@ -560,6 +561,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             wait(&p_full_bar[x][0], s_lap[x]);
                             if (!ok) break;
                             pv(x, x, 0, t == 0);
+                            umma_commit_lead(lead, &pv_half_bar[x]);
                             wait(&p_full_bar[x][1], s_lap[x]); s_lap[x] ^= 1u;
                             if (!ok) break;
                             pv(x, x, 1, false);
@@ -616,6 +618,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 wait(&p_full_bar[buf][half], lap);
                 if (!ok) break;
                 pv(x, buf, half, first && half == 0);
+                if (half == 0) umma_commit_lead(lead, &pv_half_bar[x]);
                 if (half == 1 || PARTS == 2) v_done();
             }
             if (!ok) break;
@@ -652,59 +655,55 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 tc_fence_after();
                 if (some) {
                     const uint32_t tmem_s = tmem_base + lane_base + (uint32_t)(buf * kPrefixBlock);
-                    // (Two passes over the scores in tensor memory, 64 columns at a time: holding a row's 128 in registers makes straight-line
-                    // code of 20 KB, which the first blocks of a CTA wait for instruction by instruction.)
                     const int start = r.pos0 + t * kPrefixBlock;
                     const int seen = r.tail && start + kPrefixBlock > r.L + 1 ? r.L + j - start : kPrefixBlock;      // the last column this row sees
-                    const bool masked = seen < kPrefixBlock;
-                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-                    for (int c0 = 0; c0 < kPrefixBlock; c0 += 64) {
-                        uint32_t s[64];
-                        tmem_ld_row32(tmem_s + (uint32_t)c0, s);
-                        tmem_ld_row32(tmem_s + (uint32_t)(c0 + 32), s + 32);
-                        tmem_ld_wait(s);
-                        if (masked) {
-#pragma unroll
-                            for (int c = 0; c < 64; ++c) s[c] = c0 + c > seen ? 0xff800000u : s[c];
-                        }
-#pragma unroll
-                        for (int c = 0; c < 64; c += 2) m4[(c >> 1) & 3] = max3(m4[(c >> 1) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
-                    }
-                    const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale_log2;        // (the scale is positive)
-                    // The reference moves when the row's maximum has outgrown it by the threshold; O and l follow it.
-                    float factor = 1.f;
-                    bool moved = false;
-                    if (ref == -INFINITY) ref = mx;
-                    else if (mx > ref + kRescaleThreshold) { factor = exp2f(ref - mx); ref = mx; moved = true; }
-                    if (__any_sync(0xffffffffu, moved)) {
-                        // (two accumulators: the scores stand behind the product before them, so O is up to date)
-                        if (NT == 1 && !mbar_wait_warp(&pv_done_bar, (uint32_t)(tau - 1) & 1u, abort_ptr)) { ok = false; break; }
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int c0 = 0; c0 < D; c0 += 32) {
-                            uint32_t o[32];
-                            tmem_ld_row32(tmem_o + (uint32_t)c0, o);
-                            tmem_ld_wait(o);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * factor);
-                            tmem_st_row32(tmem_o + (uint32_t)c0, o);
-                        }
-                        l_run *= factor;
-                    }
-                    const float neg = ref == -INFINITY ? 0.f : -ref;
-                    const uint64_t scale2 = pack2(scale_log2, scale_log2), neg2 = pack2(neg, neg);
+                    const uint64_t scale2 = pack2(scale_log2, scale_log2);
                     uint64_t part[4] = {0, 0, 0, 0};                   // sums of pairs
+                    // 64 columns at a time: the product with V of the first half runs under the second's exponentials, and the code is half as
+                    // long (a CTA waits for its first blocks' instructions one by one).
 #pragma unroll 1
                     for (int h = 0; h < 2; ++h) {
-                        uint32_t s[64], pk[32];
+                        uint32_t s[64];
                         tmem_ld_row32(tmem_s + (uint32_t)(h * 64), s);
                         tmem_ld_row32(tmem_s + (uint32_t)(h * 64 + 32), s + 32);
                         tmem_ld_wait(s);
-                        if (masked) {
+                        if (seen < kPrefixBlock) {
 #pragma unroll
                             for (int c = 0; c < 64; ++c) s[c] = h * 64 + c > seen ? 0xff800000u : s[c];
                         }
+                        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int c = 0; c < 64; c += 2) m4[(c >> 1) & 3] = max3(m4[(c >> 1) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                        const float mx = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]) * scale_log2;        // (the scale is positive)
+                        // The reference moves when the row's maximum has outgrown it by the threshold; O and l follow it.
+                        float factor = 1.f;
+                        bool moved = false;
+                        if (ref == -INFINITY) ref = mx;
+                        else if (mx > ref + kRescaleThreshold) { factor = exp2f(ref - mx); ref = mx; moved = true; }
+                        if (__any_sync(0xffffffffu, moved)) {
+                            // O has to be up to date: with the block's first half where this is its second, else with the block before (two
+                            // accumulators: this block's scores stand behind it)
+                            if (h == 1 && !mbar_wait_warp(&pv_half_bar[x], (uint32_t)tau & 1u, abort_ptr)) ok = false;
+                            if (h == 0 && NT == 1 && !mbar_wait_warp(&pv_done_bar, (uint32_t)(tau - 1) & 1u, abort_ptr)) ok = false;
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c0 = 0; c0 < D; c0 += 32) {
+                                uint32_t o[32];
+                                tmem_ld_row32(tmem_o + (uint32_t)c0, o);
+                                tmem_ld_wait(o);
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * factor);
+                                tmem_st_row32(tmem_o + (uint32_t)c0, o);
+                            }
+                            l_run *= factor;
+                            const uint64_t factor2 = pack2(factor, factor);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) part[k] = fma2(part[k], factor2, 0);
+                        }
+                        const float neg = ref == -INFINITY ? 0.f : -ref;
+                        const uint64_t neg2 = pack2(neg, neg);
+                        uint32_t pk[32];
 #pragma unroll
                         for (int c = 0; c < 32; ++c) {
                             const float2 e = unpack2(fma2(pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), scale2, neg2));
@@ -712,13 +711,13 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             part[c & 3] = add2(part[c & 3], pack2(p0, p1));
                             pk[c] = bf16x2(p0, p1);
                         }
-                        // (over columns that have been read: P is half as wide as S)
-                        tmem_st_row32(tmem_s + (uint32_t)(h * 32), pk);
+                        tmem_st_row32(tmem_s + (uint32_t)(h * 32), pk);       // (over columns that have been read: P is half as wide as S)
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&p_full_bar[buf][h]);
                     }
+                    if (!ok) break;
                     const float2 sum = unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])));
                     l_run += sum.x + sum.y;
                 } else {

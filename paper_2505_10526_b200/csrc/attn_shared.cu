@@ -18,8 +18,8 @@
 // blocks of all tails of a CTA form one pipeline across items (the next item's queries have a buffer of their own): the scores run two
 // blocks ahead of the weights, and where there is room for two accumulators the blocks alternate between them.
 //
-// Warps 0 and 3 copy K and V (TMA), each into a ring of its own; warp 1 issues the products; warp 2 patches the block's own K/V rows into
-// the blocks that hold their positions and stores them to their page slots; four warps per tile make the softmax.
+// Warps 0 and 3 copy K and V (TMA), each into a ring of its own; warp 1 issues the products; warp 2 and the last warp patch the block's own
+// K and V rows into the blocks that hold their positions and store them to their page slots; four warps per tile make the softmax.
 //
 // All items form one line, a block costing what its kind costs (below), cut into equal ranges for a persistent grid of one CTA per
 // SM: prefix items, which the tensor cores bound, and tails, which memory bounds, are at work at the same time.  What a CTA has
@@ -57,7 +57,7 @@ struct SharedCfg {
     static constexpr int kEntries = D == 64 ? 4 : 2;         // of each ring
     static constexpr int kBoxes = kPagesPerBlock * kNCH / kParts;      // 16-position x 64-element boxes of an entry
     static constexpr int kSmem = kTiles * kQTile + 2 * kEntries * kEntry + 1024;      // and the line (line_ints)
-    static constexpr int kThreads = 128 + kTiles * 128;
+    static constexpr int kThreads = 160 + kTiles * 128;
     static constexpr uint32_t kTmemCols = 512;
     static constexpr uint32_t kTmemO = 2 * kPrefixBlock;      // two score buffers, then the accumulators
     static constexpr int kMaxSmem = kSmem + (kSharedMaxBatch + 1 + 5 * (kMaxGroups + 1)) * 4;
@@ -184,7 +184,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (threadIdx.x == 0) {
         for (int e = 0; e < 2 * E; ++e) { mbar_init(&ready_bar[e], 1); mbar_init(&empty_bar[e], 1); mbar_init(&landed_bar[e], 1); }
         mbar_init(&pv_done_bar, 1); mbar_init(&pv_half_bar[0], 1); mbar_init(&pv_half_bar[1], 1);
-        for (int i = 0; i < kRunQueue; ++i) { mbar_init(&run_ready_bar[i], 1); mbar_init(&run_free_bar[i], 3 + 4 * NT); }      // V, helper, products, softmax
+        for (int i = 0; i < kRunQueue; ++i) { mbar_init(&run_ready_bar[i], 1); mbar_init(&run_free_bar[i], 4 + 4 * NT); }      // V, two helpers, products, softmax
         for (int i = 0; i < 2; ++i) { mbar_init(&q_ready_bar[i], 1); mbar_init(&q_free_bar[i], 1); mbar_init(&s_full_bar[i], 1); mbar_init(&p_full_bar[i][0], 4); mbar_init(&p_full_bar[i][1], 4); mbar_init(&o_full_bar[i], 1); mbar_init(&o_free_bar[i], 4); }
         abort_flag = 0;
         s_bad = 0;
@@ -425,16 +425,16 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         if (lane == 0 && *abort_ptr) {
             for (int i = 0; i < 64; ++i) __nanosleep(2000);            // let copies in flight land
         }
-    } else if (warp == 2) {
-        // ------------------------------------------------ helper: the block's own rows, and what lies behind the last position
+    } else if (warp == 2 || warp == 4 + 4 * NT) {
+        // ------------------------------------------------ helpers: the block's own rows, and what lies behind the last position
+        const bool is_v = warp != 2;
         uint32_t landed_phase = 0;       // bit e: parity of the next completion of landed_bar[e]
-        int ring_at[2] = {0, 0};         // entries of each ring so far
+        int it = 0;                      // entries of the ring so far
         bool ok = true;
-        // One block's K or V, entry by entry.
-        auto patch = [&](const Run& r, int t, bool is_v) {
+        Run r;
+        // Block t of the run, entry by entry.
+        auto patch = [&](int t) {
             const int start = r.pos0 + t * kPrefixBlock, end = r.L + R;
-            int& it = ring_at[is_v ? 1 : 0];
-            if (!r.tail || start + kPrefixBlock <= r.L) { it += PARTS; return; }
             const int32_t* pt = p.a.page_table + (size_t)r.seq * p.a.max_pages;
             const __nv_bfloat16* src = is_v ? p.a.v_new : p.a.k_new;
             __nv_bfloat16* pool = is_v ? p.a.v_pages : p.a.k_pages;
@@ -485,24 +485,10 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 if (lane == 0) mbar_arrive(&ready_bar[e]);
             }
         };
-        // K runs ahead of V as the scores do
-        struct Blocks { Run r; int run, t; };
-        Blocks k, v;
-        k.run = 0; k.t = 0;
-        bool any = take_run(0, k.r, true);
-        v = k;
-        bool have_v = any;
-        for (int ahead = 0; have_v && ok;) {
-            const bool is_v = !(any && ahead < 2);
-            Blocks& w = is_v ? v : k;
-            patch(w.r, w.t, is_v);
-            if (++w.t == w.r.n) {
-                if (is_v && lane == 0) mbar_arrive(&run_free_bar[v.run % kRunQueue]);
-                w.t = 0;
-                const bool more = take_run(++w.run, w.r, true);
-                if (is_v) have_v = more; else any = more;
-            }
-            ahead += is_v ? -1 : 1;
+        for (int run = 0; ok && take_run(run, r, false); ++run) {
+            const int t0 = r.tail ? min(r.n, max(0, r.L - r.pos0) / kPrefixBlock) : r.n;       // the first block with a position not in the cache
+            it += t0 * PARTS;
+            for (int t = t0; t < r.n && ok; ++t) patch(t);
         }
     } else if (warp == 1) {
         // ------------------------------------------------ products

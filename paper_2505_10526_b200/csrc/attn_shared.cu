@@ -37,7 +37,7 @@ constexpr int kPagesPerBlock = kPrefixBlock / kPageSize;
 constexpr float kRescaleThreshold = 8.f;   // log2 units a row's maximum may outgrow its reference by
 
 // Cost of a block: products of two tiles, of one, of a tail; and what an item costs beside its blocks (queries, write-out).
-constexpr int kCostTwo = 8, kCostOne = 5, kCostTail = 4, kCostPrefixItem = 8, kCostTailItem = 4;
+constexpr int kCostTwo = 8, kCostOne = 7, kCostTail = 7, kCostPrefixItem = 8, kCostTailItem = 5;
 constexpr int kCostMost = kCostTwo + kCostPrefixItem;
 
 // Blocks of an item that begins at `start`: block 0 there, block k > 0 at start + item + k * block.  The first block that begins at or
@@ -81,6 +81,20 @@ __device__ __forceinline__ void tmem_ld_row32(uint32_t taddr, uint32_t* r) {
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr));
 }
+__device__ __forceinline__ void tmem_ld_row16(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st_row16(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
+        "r"(r[14]), "r"(r[15])
+        : "memory");
+}
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 template <int N>
 __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[N]) {
@@ -88,40 +102,23 @@ __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[N]) {
 #pragma unroll
     for (int j = 0; j < N; ++j) asm volatile("" : "+r"(r[j]));       // no use may move ahead of the wait
 }
-__device__ __forceinline__ void tmem_st_row32(uint32_t taddr, const uint32_t* r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
-        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
-        "r"(r[31])
-        : "memory");
-}
 
 // Where a piece is kept: slots of the CTAs' cut items (two each), slots of prefix items that one CTA has all of, slots of such tails.
-struct Piece {
-    float4* o;            // [d / 4][stride rows]: unit c4 * stride + row holds four columns of a row
-    float2* ml;           // [stride rows]: reference (log2 units) and sum
-    int stride;
-};
-__device__ __forceinline__ Piece piece_at(const SharedAttnParams& p, int slot, int x, int D) {
+// The number of rows of the pieces ahead of it, and how many it has itself.  A piece's values are [d / 4][rows] groups of four
+// columns, its references (log2 units) and sums [rows] pairs.
+__device__ __forceinline__ long long piece_rows(const SharedAttnParams& p, int slot, int x, int& n_rows) {
     const SharedAttnSlots& s = p.slots;
-    const int big = s.cut + s.prefix_items, item = -1 - slot;
-    size_t rows;                                                       // rows of the pieces ahead of it
-    Piece r;
-    r.stride = kTileRows;
-    if (slot >= 0) rows = ((size_t)slot * s.tiles + x) * kTileRows;
-    else if (item < s.prefix_items) rows = ((size_t)(s.cut + item) * s.tiles + x) * kTileRows;
+    const int item = -1 - slot;
+    long long rows;
+    n_rows = kTileRows;
+    if (slot >= 0) rows = ((long long)slot * s.tiles + x) * kTileRows;
+    else if (item < s.prefix_items) rows = ((long long)(s.cut + item) * s.tiles + x) * kTileRows;
     else {
-        rows = (size_t)big * s.tiles * kTileRows + ((size_t)(item - s.prefix_items) * s.tiles + x) * s.tail_rows;
-        r.stride = s.tail_rows;
+        n_rows = s.tail_rows;
+        rows = (long long)(s.cut + s.prefix_items) * s.tiles * kTileRows + ((long long)(item - s.prefix_items) * s.tiles + x) * n_rows;
     }
-    if (!MASSV_IN_BOUNDS(rows + r.stride, (long long)s.rows() + 1, p.a.dev_status)) rows = 0;
-    r.o = reinterpret_cast<float4*>(p.part_o) + rows * (D / 4);
-    r.ml = reinterpret_cast<float2*>(p.part_ml) + rows;
-    return r;
+    if (!MASSV_IN_BOUNDS(rows + n_rows, (long long)s.rows() + 1, p.a.dev_status)) rows = 0;
+    return rows;
 }
 
 // ---- the line of work, in shared memory: what every role finds its pieces by
@@ -431,9 +428,8 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         uint32_t landed_phase = 0;       // bit e: parity of the next completion of landed_bar[e]
         int it = 0;                      // entries of the ring so far
         bool ok = true;
-        Run r;
-        // Block t of the run, entry by entry.
-        auto patch = [&](int t) {
+        // Block t of a run, entry by entry.
+        auto patch = [&](const Run& r, int t) {
             const int start = r.pos0 + t * kPrefixBlock, end = r.L + R;
             const int32_t* pt = p.a.page_table + (size_t)r.seq * p.a.max_pages;
             const __nv_bfloat16* src = is_v ? p.a.v_new : p.a.k_new;
@@ -485,10 +481,11 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 if (lane == 0) mbar_arrive(&ready_bar[e]);
             }
         };
+        Run r;
         for (int run = 0; ok && take_run(run, r, false); ++run) {
             const int t0 = r.tail ? min(r.n, max(0, r.L - r.pos0) / kPrefixBlock) : r.n;       // the first block with a position not in the cache
             it += t0 * PARTS;
-            for (int t = t0; t < r.n && ok; ++t) patch(t);
+            for (int t = t0; t < r.n && ok; ++t) patch(r, t);
         }
     } else if (warp == 1) {
         // ------------------------------------------------ products
@@ -661,43 +658,47 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
                         for (int c = 0; c < 64; c += 2) m4[(c >> 1) & 3] = max3(m4[(c >> 1) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
                         const float mx = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]) * scale_log2;        // (the scale is positive)
-                        // The reference moves when the row's maximum has outgrown it by the threshold; O and l follow it.
-                        float factor = 1.f;
-                        bool moved = false;
-                        if (ref == -INFINITY) ref = mx;
-                        else if (mx > ref + kRescaleThreshold) { factor = exp2f(ref - mx); ref = mx; moved = true; }
-                        if (__any_sync(0xffffffffu, moved)) {
-                            // O has to be up to date: with the block's first half where this is its second, else with the block before (two
-                            // accumulators: this block's scores stand behind it)
-                            if (h == 1 && !mbar_wait_warp(&pv_half_bar[x], (uint32_t)tau & 1u, abort_ptr)) ok = false;
-                            if (h == 0 && NT == 1 && !mbar_wait_warp(&pv_done_bar, (uint32_t)(tau - 1) & 1u, abort_ptr)) ok = false;
-                            if (!ok) break;
-                            tc_fence_after();
+                        // The reference moves when the row's maximum has outgrown it by the threshold (and when it is first set); O and l follow it.
+                        if (__any_sync(0xffffffffu, mx > ref + kRescaleThreshold)) {
+                            const bool moved = mx > ref + kRescaleThreshold;
+                            const float factor = moved && ref != -INFINITY ? exp2f(ref - mx) : 1.f;
+                            ref = moved ? mx : ref;
+                            if (__any_sync(0xffffffffu, factor != 1.f)) {
+                                // O has to be up to date: with the block's first half where this is its second, else with the block before (two
+                                // accumulators: this block's scores stand behind it)
+                                if (h == 1 && !mbar_wait_warp(&pv_half_bar[x], (uint32_t)tau & 1u, abort_ptr)) ok = false;
+                                if (h == 0 && NT == 1 && !mbar_wait_warp(&pv_done_bar, (uint32_t)(tau - 1) & 1u, abort_ptr)) ok = false;
+                                if (!ok) break;
+                                tc_fence_after();
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 32) {
-                                uint32_t o[32];
-                                tmem_ld_row32(tmem_o + (uint32_t)c0, o);
-                                tmem_ld_wait(o);
+                                for (int c0 = 0; c0 < D; c0 += 16) {
+                                    uint32_t o[16];
+                                    tmem_ld_row16(tmem_o + (uint32_t)c0, o);
+                                    tmem_ld_wait(o);
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * factor);
-                                tmem_st_row32(tmem_o + (uint32_t)c0, o);
+                                    for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * factor);
+                                    tmem_st_row16(tmem_o + (uint32_t)c0, o);
+                                }
+                                l_run *= factor;
+                                const uint64_t factor2 = pack2(factor, factor);
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) part[k] = fma2(part[k], factor2, 0);
                             }
-                            l_run *= factor;
-                            const uint64_t factor2 = pack2(factor, factor);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) part[k] = fma2(part[k], factor2, 0);
                         }
                         const float neg = ref == -INFINITY ? 0.f : -ref;
                         const uint64_t neg2 = pack2(neg, neg);
-                        uint32_t pk[32];
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            const float2 e = unpack2(fma2(pack2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), scale2, neg2));
-                            const float p0 = ex2_ftz(e.x), p1 = ex2_ftz(e.y);
-                            part[c & 3] = add2(part[c & 3], pack2(p0, p1));
-                            pk[c] = bf16x2(p0, p1);
+                        for (int c0 = 0; c0 < 64; c0 += 32) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) {
+                                const float2 e = unpack2(fma2(pack2(__uint_as_float(s[c0 + 2 * c]), __uint_as_float(s[c0 + 2 * c + 1])), scale2, neg2));
+                                const float p0 = ex2_ftz(e.x), p1 = ex2_ftz(e.y);
+                                part[c & 3] = add2(part[c & 3], pack2(p0, p1));
+                                pk[c] = bf16x2(p0, p1);
+                            }
+                            tmem_st_row16(tmem_s + (uint32_t)(h * 32 + c0 / 2), pk);       // (over columns that have been read: P is half as wide as S)
                         }
-                        tmem_st_row32(tmem_s + (uint32_t)(h * 32), pk);       // (over columns that have been read: P is half as wide as S)
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                         tc_fence_before();
                         __syncwarp();
@@ -716,7 +717,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             tc_fence_after();
             if (some) {
                 // ---- the piece
-                const Piece pc = piece_at(p, r.slot, turn, D);
+                int stride;
+                const long long base = piece_rows(p, r.slot, turn, stride);
+                float4* dst = reinterpret_cast<float4*>(p.part_o) + base * (D / 4) + row;
                 const bool live = row < r.n_rows[x];
 #pragma unroll 1
                 for (int c0 = 0; c0 < D; c0 += 32) {
@@ -726,11 +729,10 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     if (live) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
-                            pc.o[(size_t)((c0 + k) / 4) * pc.stride + row] =
-                                make_float4(__uint_as_float(o[k]), __uint_as_float(o[k + 1]), __uint_as_float(o[k + 2]), __uint_as_float(o[k + 3]));
+                            dst[(size_t)((c0 + k) / 4) * stride] = make_float4(__uint_as_float(o[k]), __uint_as_float(o[k + 1]), __uint_as_float(o[k + 2]), __uint_as_float(o[k + 3]));
                     }
                 }
-                if (live) pc.ml[row] = make_float2(ref, l_run);
+                if (live) reinterpret_cast<float2*>(p.part_ml)[base + row] = make_float2(ref, l_run);
             }
             tc_fence_before();
             __syncwarp();
@@ -749,59 +751,114 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     if (threadIdx.x == 0 && abort_flag) set_status(p.a.dev_status, MASSV_ERR_TIMEOUT);
 }
 
-// Pieces of a row added up.  CTA (sequence and KV head, part of its units): a unit is eight columns of one row, rows side by side.
-constexpr int kMergeThreads = 128;
-__global__ void __launch_bounds__(kMergeThreads) attn_shared_merge_kernel(const SharedAttnParams p, int tiles_per_item) {
+// Pieces of a row added up.  A unit is eight columns of one query row of a (sequence, KV head) pair, rows side by side.  A thread goes through
+// its unit's pieces four at a time, all their loads in flight together, with a running maximum; where there are few units, eight threads
+// share one, each taking every eighth four.  The order of the sums is fixed.
+template <int SHARE>
+__global__ void __launch_bounds__(SHARE == 1 ? 128 : 256) attn_shared_merge_kernel(const SharedAttnParams p) {
+    constexpr int kUnits = SHARE == 1 ? 128 : 256 / SHARE;             // of a CTA
+    __shared__ float s_red[SHARE == 1 ? 1 : 10][SHARE == 1 ? 1 : 256];
     const int h = blockIdx.x % p.a.Hkv, b = blockIdx.x / p.a.Hkv, D = p.a.d, R = p.a.R;
-    const int G = p.a.Hq / p.a.Hkv, rows = G * R, nb = kTileRows / G;
-    const int unit = blockIdx.y * kMergeThreads + threadIdx.x, row = unit % rows, c8 = unit / rows;
+    const int G = p.a.Hq / p.a.Hkv, rows = G * R, nb = kTileRows / G, share = threadIdx.x / kUnits;
+    const int unit = blockIdx.y * kUnits + threadIdx.x % kUnits, c8 = unit / rows, row = unit - c8 * rows;
+    const SharedAttnSlots& sl = p.slots;
+    const int j = row / G, hh = row - j * G;
     pdl_wait();
     pdl_trigger();
     const int4 seq = p.seqs[b], grp = p.seq_groups[b];
     const int per = p.meta[0], tails0 = p.meta[1];
-    if (seq.y <= 0 || c8 * 8 >= D) return;                             // skipped; past the last unit
+    if (seq.y <= 0) return;                            // a sequence without room
+    const bool live = c8 * 8 < D;
     // An item's pieces: consecutive CTAs of the kernel above; alone in one, it has a slot of its own.
     struct Pieces { int start, c0, c1, item; };
     auto pieces_of = [&](int start, int blocks, int cost, int extra, int item) { return Pieces{start, start / per, block_begin(blocks - 1, start, cost, extra) / per, item}; };
     auto slot_of = [&](const Pieces& q, int c) { return q.c0 == q.c1 ? -1 - q.item : c * 2 + (q.start < c * per ? 0 : 1); };
-    const Pieces tl = pieces_of(tails0 + seq.x * p.a.Hkv + h * (seq.y * kCostTail + kCostTailItem), seq.y, kCostTail, kCostTailItem, p.slots.prefix_items + b * p.a.Hkv + h);
-    const int pair = seq.z + row / G, tile = pair / nb, k = tile / tiles_per_item * p.a.Hkv + h;
-    const int prow = (pair - tile * nb) * G + row % G, px = tile % tiles_per_item;
+    const Pieces tl = pieces_of(tails0 + seq.x * p.a.Hkv + h * (seq.y * kCostTail + kCostTailItem), seq.y, kCostTail, kCostTailItem, sl.prefix_items + b * p.a.Hkv + h);
+    const int pair = seq.z + j, tile = pair / nb, at_prefix = (pair - tile * nb) * G + hh, tiles = sl.tiles;
     Pieces pf{0, 0, -1, 0};
-    if (seq.w > 0) pf = pieces_of(grp.x + k * (seq.w * grp.z + kCostPrefixItem), seq.w, grp.z, kCostPrefixItem, grp.y + k);
-    // a tail's piece is in two accumulators where it has more than one block
-    auto tail_tiles = [&](int c) {
-        const int k0 = first_block(c * per, tl.start, kCostTail, kCostTailItem), k1 = min(seq.y, first_block((c + 1) * per, tl.start, kCostTail, kCostTailItem));
-        return min(tiles_per_item, k1 - k0);
-    };
-    float m = -INFINITY;
-    for (int c = pf.c0; c <= pf.c1; ++c) m = fmaxf(m, piece_at(p, slot_of(pf, c), px, D).ml[prow].x);
-    for (int c = tl.c0; c <= tl.c1; ++c)
-        for (int x = 0; x < tail_tiles(c); ++x) m = fmaxf(m, piece_at(p, slot_of(tl, c), x, D).ml[row].x);
-    float sum = 0.f, acc[8] = {};
-    auto add = [&](const Piece& pc, int at) {
-        const float2 ml = pc.ml[at];
-        const float4 u = pc.o[(size_t)(2 * c8) * pc.stride + at], v = pc.o[(size_t)(2 * c8 + 1) * pc.stride + at];
-        const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);     // (a row that sees nothing of the piece)
-        sum += ml.y * w;
-        acc[0] += u.x * w; acc[1] += u.y * w; acc[2] += u.z * w; acc[3] += u.w * w;
-        acc[4] += v.x * w; acc[5] += v.y * w; acc[6] += v.z * w; acc[7] += v.w * w;
-    };
-#pragma unroll 4
-    for (int c = pf.c0; c <= pf.c1; ++c) add(piece_at(p, slot_of(pf, c), px, D), prow);
-    for (int c = tl.c0; c <= tl.c1; ++c)
-        for (int x = 0; x < tail_tiles(c); ++x) add(piece_at(p, slot_of(tl, c), x, D), row);
+    if (seq.w > 0) {
+        const int k = tile / tiles * p.a.Hkv + h;
+        pf = pieces_of(grp.x + k * (seq.w * grp.z + kCostPrefixItem), seq.w, grp.z, kCostPrefixItem, grp.y + k);
+    }
+    const int n_prefix = pf.c1 - pf.c0 + 1, n_pieces = live ? n_prefix + (tl.c1 - tl.c0 + 1) * tiles : 0;
+    const float4* po = reinterpret_cast<const float4*>(p.part_o);
+    const float2* pml = reinterpret_cast<const float2*>(p.part_ml);
+    float M = -INFINITY, sum = 0.f, acc[8] = {};
+    for (int first = share * 4; first < n_pieces; first += 4 * SHARE) {
+        float2 ml[4];
+        float4 u[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = first + i;
+            ml[i] = make_float2(-INFINITY, 0.f);
+            u[i] = v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            int slot = 0, x = tile & (tiles - 1), at = at_prefix;
+            bool have = k < n_pieces;
+            if (k < n_prefix) {
+                slot = slot_of(pf, pf.c0 + k);
+            } else if (have) {
+                // a tail's piece is in two accumulators where it has more than one block
+                const int w = k - n_prefix, c = tl.c0 + w / tiles;
+                x = w & (tiles - 1);
+                slot = slot_of(tl, c);
+                at = row;
+                if (x > 0) have = min(seq.y, first_block((c + 1) * per, tl.start, kCostTail, kCostTailItem)) - first_block(c * per, tl.start, kCostTail, kCostTailItem) > 1;
+            }
+            if (have) {
+                int stride;
+                const long long base = piece_rows(p, slot, x, stride);
+                ml[i] = pml[base + at];
+                const float4* o = po + base * (D / 4) + (long long)(2 * c8) * stride + at;
+                u[i] = o[0];
+                v[i] = o[stride];
+            }
+        }
+        const float m = fmaxf(M, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+        const float keep = M == -INFINITY ? 0.f : exp2f(M - m);
+        M = m;
+        sum *= keep;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] *= keep;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float w = ml[i].x == -INFINITY ? 0.f : exp2f(ml[i].x - m);       // (a row may see nothing of a piece)
+            sum += ml[i].y * w;
+            acc[0] += u[i].x * w; acc[1] += u[i].y * w; acc[2] += u[i].z * w; acc[3] += u[i].w * w;
+            acc[4] += v[i].x * w; acc[5] += v[i].y * w; acc[6] += v[i].z * w; acc[7] += v[i].w * w;
+        }
+    }
+    if constexpr (SHARE > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s_red[i][threadIdx.x] = acc[i];
+        s_red[8][threadIdx.x] = sum;
+        s_red[9][threadIdx.x] = M;
+        __syncthreads();
+        if (share != 0) return;
+        for (int g = 1; g < SHARE; ++g) M = fmaxf(M, s_red[9][g * kUnits + threadIdx.x]);
+        const float own = s_red[9][threadIdx.x] == -INFINITY ? 0.f : exp2f(s_red[9][threadIdx.x] - M);
+        sum *= own;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] *= own;
+        for (int g = 1; g < SHARE; ++g) {
+            const int from = g * kUnits + threadIdx.x;
+            const float w = s_red[9][from] == -INFINITY ? 0.f : exp2f(s_red[9][from] - M);
+            sum += s_red[8][from] * w;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += s_red[i][from] * w;
+        }
+    }
+    if (!live) return;
     const float inv = 1.f / sum;
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] *= inv;
-    const size_t out = ((size_t)b * R + row / G) * p.a.Hq + h * G + row % G;
+    const size_t out = ((size_t)b * R + j) * p.a.Hq + h * G + hh;
     *reinterpret_cast<uint4*>(p.a.out + out * D + c8 * 8) = make_uint4(bf16x2(acc[0], acc[1]), bf16x2(acc[2], acc[3]), bf16x2(acc[4], acc[5]), bf16x2(acc[6], acc[7]));
     if (p.a.out_f32) {
         float4* f = reinterpret_cast<float4*>(p.a.out_f32 + out * D + c8 * 8);
         f[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
         f[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
     }
-    if (p.a.lse && c8 == 0) p.a.lse[out] = (m + log2f(sum)) * 0.6931471805599453f;
+    if (p.a.lse && c8 == 0) p.a.lse[out] = (M + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <int D>
@@ -821,8 +878,9 @@ cudaError_t launch(const SharedAttnParams& p, cudaStream_t stream) {
     const size_t smem = Cfg::kSmem + (size_t)(p.a.B + 1 + 5 * (p.n_groups + 1)) * 4;
     e = launch_pdl(attn_shared_kernel<D>, dim3(ctas), dim3(Cfg::kThreads), smem, stream, mk, mv, mq, mqt, p);
     if (e != cudaSuccess) return e;
-    const int units = G * p.a.R * (D / 8);
-    return launch_pdl(attn_shared_merge_kernel, dim3(p.a.B * p.a.Hkv, (units + kMergeThreads - 1) / kMergeThreads), dim3(kMergeThreads), 0, stream, p, Cfg::kTiles);
+    const int pairs = p.a.B * p.a.Hkv, units = G * p.a.R * (D / 8);
+    if ((long)pairs * units * 8 > 512L * ctas) return launch_pdl(attn_shared_merge_kernel<1>, dim3(pairs, (units + 127) / 128), dim3(128), 0, stream, p);
+    return launch_pdl(attn_shared_merge_kernel<8>, dim3(pairs, (units + 31) / 32), dim3(256), 0, stream, p);
 }
 
 }  // namespace

@@ -173,18 +173,24 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __shared__ __align__(8) uint64_t run_ready_bar[kRunQueue], run_free_bar[kRunQueue];      // the runs, worked out by the K warp for all
     __shared__ Run s_runs[kRunQueue];
     __shared__ uint32_t tmem_base_slot;
-    __shared__ int abort_flag, s_bad;
+    __shared__ int abort_flag;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int R = p.a.R, B = p.a.B, cap = p.a.max_pages * kPageSize;
     const int G = p.a.Hq / p.a.Hkv, nb = kTileRows / G, tile_rows = nb * G;
-    if (threadIdx.x == 0) {
-        for (int e = 0; e < 2 * E; ++e) { mbar_init(&ready_bar[e], 1); mbar_init(&empty_bar[e], 1); mbar_init(&landed_bar[e], 1); }
-        mbar_init(&pv_done_bar, 1); mbar_init(&pv_half_bar[0], 1); mbar_init(&pv_half_bar[1], 1);
-        for (int i = 0; i < kRunQueue; ++i) { mbar_init(&run_ready_bar[i], 1); mbar_init(&run_free_bar[i], 4 + 4 * NT); }      // V, two helpers, products, softmax
-        for (int i = 0; i < 2; ++i) { mbar_init(&q_ready_bar[i], 1); mbar_init(&q_free_bar[i], 1); mbar_init(&s_full_bar[i], 1); mbar_init(&p_full_bar[i][0], 4); mbar_init(&p_full_bar[i][1], 4); mbar_init(&o_full_bar[i], 1); mbar_init(&o_free_bar[i], 4); }
-        abort_flag = 0;
-        s_bad = 0;
+    // barriers, one thread each (45 initialisations by one thread take 1,100 cycles)
+    {
+        struct { uint64_t* bar; int n, arrivals; } const kinds[] = {
+            {ready_bar, 2 * E, 1}, {empty_bar, 2 * E, 1}, {landed_bar, 2 * E, 1}, {q_ready_bar, 2, 1}, {q_free_bar, 2, 1}, {s_full_bar, 2, 1}, {&p_full_bar[0][0], 4, 4},
+            {o_full_bar, 2, 1}, {o_free_bar, 2, 4}, {&pv_done_bar, 1, 1}, {pv_half_bar, 2, 1}, {run_ready_bar, kRunQueue, 1},
+            {run_free_bar, kRunQueue, 4 + 4 * NT}};                   // V, two helpers, products, softmax
+        int at = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(kinds) / sizeof(kinds[0])); ++i) {
+            if (at >= 0 && at < kinds[i].n) mbar_init(kinds[i].bar + at, kinds[i].arrivals);
+            at -= kinds[i].n;
+        }
+        if (threadIdx.x == 0) abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -212,18 +218,22 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
     // ---- groups: the least length of the members and their number (gcost, gitem for the moment), the first sequence
     auto fits = [&](int L) { return L >= 0 && L + R <= cap; };
-    for (int i = threadIdx.x; i <= p.n_groups; i += blockDim.x) {
-        const int lo = p.group_start[i];
-        gs[i] = lo;
-        if (i < p.n_groups) { gcost[i] = 0x7fffffff; gitem[i] = 0; gsrc[i] = 0x7fffffff; gblocks[i] = p.shared_lens[i]; }
-        if ((i == 0 && lo != 0) || (i == p.n_groups && lo != B) || (i < p.n_groups && lo > p.group_start[i + 1])) s_bad = 1;
+    bool bad_here = false;
+    {
+        // (the first round's loads are all asked for before any is used)
+        const int t = threadIdx.x, n = p.n_groups;
+        const int L0 = t < B ? p.a.seq_lens[t] : 0, g0 = t <= n ? p.group_start[t] : 0, g1 = t < n ? p.group_start[t + 1] : 0, sh = t < n ? p.shared_lens[t] : 0;
+        if (t <= n) gs[t] = g0;
+        if (t < n) { gcost[t] = 0x7fffffff; gitem[t] = 0; gsrc[t] = 0x7fffffff; gblocks[t] = sh; }
+        bad_here = (t == 0 && g0 != 0) || (t == n && g0 != B) || (t < n && g0 > g1);
+        if (t < B) tail[t + 1] = L0;
+        for (int b = t + blockDim.x; b < B; b += blockDim.x) tail[b + 1] = p.a.seq_lens[b];
     }
-    for (int b = threadIdx.x; b < B; b += blockDim.x) tail[b + 1] = p.a.seq_lens[b];
-    __syncthreads();
-    const bool bad = s_bad != 0;
-    if (bad)                                // one group that shares nothing
+    const bool bad = __syncthreads_or(bad_here) != 0;      // (at most 256 groups: one round)
+    if (bad) {                              // one group that shares nothing
         for (int i = threadIdx.x; i <= p.n_groups; i += blockDim.x) { gs[i] = i == 0 ? 0 : B; if (i < p.n_groups) gblocks[i] = 0; }
-    __syncthreads();
+        __syncthreads();
+    }
     for (int b = threadIdx.x; b < B; b += blockDim.x) {
         const int L = tail[b + 1], g = find_last(gs, p.n_groups, b);
         if (!fits(L)) continue;
@@ -232,43 +242,46 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         atomicAdd(&gitem[g], 1);
     }
     __syncthreads();
-    // whole blocks that every member has committed; a sequence alone shares nothing
-    for (int i0 = 0; i0 < p.n_groups; i0 += blockDim.x) {              // (one round: at most 256 groups)
-        const int i = i0 + threadIdx.x;
-        if (i < p.n_groups) gblocks[i] = gitem[i] < 2 ? 0 : max(0, min(gblocks[i], gcost[i])) / kPrefixBlock;
+    {
+        // whole blocks that every member has committed; a sequence alone shares nothing
+        const int i = threadIdx.x;
+        int items = 0, cost = 0;
+        if (i < p.n_groups) {
+            const int blocks = gitem[i] < 2 ? 0 : max(0, min(gblocks[i], gcost[i])) / kPrefixBlock;
+            const int pairs = (gs[i + 1] - gs[i]) * R, tiles = (pairs + nb - 1) / nb;
+            gblocks[i] = blocks;
+            items = blocks > 0 ? (tiles + NT - 1) / NT * p.a.Hkv : 0;
+            cost = items * (blocks * (NT == 2 && tiles > 1 ? kCostTwo : kCostOne) + kCostPrefixItem);
+        }
+        __syncthreads();
+        if (i < p.n_groups) { gitem[i + 1] = items; gcost[i + 1] = cost; }
+        if (i == 0) { gcost[0] = 0; gitem[0] = 0; tail[0] = 0; }
     }
-    __syncthreads();
     for (int b = threadIdx.x; b < B; b += blockDim.x) {
         const int L = tail[b + 1];
         const bool ok = fits(L);
         if (!ok && blockIdx.x == 0) set_status(p.a.dev_status, MASSV_ERR_CAPACITY);
         tail[b + 1] = ok ? ((L + R + kPrefixBlock - 1) / kPrefixBlock - gblocks[find_last(gs, p.n_groups, b)]) * kCostTail + kCostTailItem : 0;
     }
-    for (int i = threadIdx.x; i < p.n_groups; i += blockDim.x) {
-        const int pairs = (gs[i + 1] - gs[i]) * R, tiles = (pairs + nb - 1) / nb, items = gblocks[i] > 0 ? (tiles + NT - 1) / NT * p.a.Hkv : 0;
-        gitem[i + 1] = items;
-        gcost[i + 1] = items * (gblocks[i] * (NT == 2 && tiles > 1 ? kCostTwo : kCostOne) + kCostPrefixItem);
-    }
-    if (threadIdx.x == 0) { gcost[0] = 0; gitem[0] = 0; tail[0] = 0; }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    auto scan = [&](int* cum, int n) {      // cum[1 .. n] to their running sums, by one warp
-        const int per = (n + 31) / 32, i0 = min(n, lane * per), i1 = min(n, i0 + per);
-        int local = 0;
-        for (int i = i0; i < i1; ++i) local += cum[i + 1];
-        int incl = local;
+    if (warp == 0 || warp == 2 || warp == 3) {      // running sums of cum[1 .. n], one warp each, 32 at a time
+        int* cum = warp == 0 ? gcost : warp == 2 ? gitem : tail;
+        const int n = warp == 3 ? B : p.n_groups;
+        int run = 0;
+        for (int i0 = 1; i0 <= n; i0 += 32) {
+            const int i = i0 + lane;
+            int incl = i <= n ? cum[i] : 0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += v;
+            }
+            if (i <= n) cum[i] = run + incl;
+            run += __shfl_sync(0xffffffffu, incl, 31);
         }
-        int run = incl - local;
-        for (int i = i0; i < i1; ++i) { run += cum[i + 1]; cum[i + 1] = run; }
-    };
-    if (warp == 0) scan(gcost, p.n_groups);
-    else if (warp == 2) scan(gitem, p.n_groups);
-    else if (warp == 3) scan(tail, B);
+    }
     __syncthreads();
     const int tails0 = gcost[p.n_groups];                              // where the tails begin on the line
     const int total = tails0 + tail[B] * p.a.Hkv;

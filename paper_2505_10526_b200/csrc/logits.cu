@@ -32,10 +32,35 @@ __global__ void __launch_bounds__(kMaxWarps * 32) logit_rules_kernel(const Logit
     pdl_trigger();
 
     if (p.repetition && blockIdx.x == 0 && threadIdx.x == 0 && !(p.repetition[b] > 0.f)) set_status(p.dev_status, MASSV_ERR_INVALID_ARG);
+
+    // ---- what the masks say, then the logits of allowed tokens, all requested ahead of what follows
+    const size_t row = (size_t)b * p.R + j;
+    const float* z = p.logits + row * p.V + v0;
+    const int valid = max(0, min(kLogitSlice, p.V - v0));          // (none: past the last slice)
+    const int word = v0 / 32 + lane;
+    const bool has_word = word < W;
+    const uint32_t allowed = p.allowed && has_word ? p.allowed[row * W + word] : 0xffffffffu;
+    const uint32_t prompt = p.prompt_bits && has_word ? p.prompt_bits[(size_t)b * W + word] : 0u;
+    const uint32_t output = p.output_bits && has_word ? p.output_bits[(size_t)b * W + word] : 0u;
+    int k0 = p.bias_start ? p.bias_start[b] : 0, k1 = p.bias_start ? p.bias_start[b + 1] : 0;
+    float x[kVecs][4];
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+        const uint32_t nib = (__shfl_sync(0xffffffffu, allowed, k * 4 + lane / 8) >> (lane % 8 * 4)) & 15u;
+        const int e0 = k * 128 + lane * 4;
+        if constexpr (VEC4) {
+            float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            if (nib && e0 < valid) v = *reinterpret_cast<const float4*>(z + e0);
+            x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[k][e] = nib && e0 + e < valid ? z[e0 + e] : -INFINITY;
+        }
+    }
+
     // ---- the sequence's biases that fall into this CTA's slices
     int bias_n = 0;
     if (p.bias_start) {
-        int k0 = p.bias_start[b], k1 = p.bias_start[b + 1];
         if (k0 < 0 || k1 < k0 || k1 > p.n_bias) {
             if (blockIdx.x == 0 && threadIdx.x == 0) set_status(p.dev_status, MASSV_ERR_INVALID_ARG);
             k0 = max(0, min(k0, p.n_bias)); k1 = max(k0, min(k1, p.n_bias));
@@ -57,34 +82,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32) logit_rules_kernel(const Logit
             __syncthreads();
         }
     }
-    if (v0 >= p.V) return;                                         // (no barrier behind this)
-
-    const size_t row = (size_t)b * p.R + j;
-    const float* z = p.logits + row * p.V + v0;
-    const int valid = min(kLogitSlice, p.V - v0);
-    const int word = v0 / 32 + lane;
-    const bool has_word = word < W;
-    const uint32_t allowed = p.allowed && has_word ? p.allowed[row * W + word] : 0xffffffffu;
-
-    // ---- the logits of allowed tokens, all requested ahead of what follows
-    float x[kVecs][4];
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-        const uint32_t nib = (__shfl_sync(0xffffffffu, allowed, k * 4 + lane / 8) >> (lane % 8 * 4)) & 15u;
-        const int e0 = k * 128 + lane * 4;
-        if constexpr (VEC4) {
-            float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-            if (nib && e0 < valid) v = *reinterpret_cast<const float4*>(z + e0);
-            x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[k][e] = nib && e0 + e < valid ? z[e0 + e] : -INFINITY;
-        }
-    }
+    if (valid == 0) return;                                        // (no barrier behind this)
 
     // ---- the marked tokens of this lane's word
-    const uint32_t prompt = p.prompt_bits && has_word ? p.prompt_bits[(size_t)b * W + word] : 0u;
-    const uint32_t output = p.output_bits && has_word ? p.output_bits[(size_t)b * W + word] : 0u;
     const uint32_t biased = bias_n > 0 ? bias_bits[local * kWords + lane] : 0u;
     uint32_t drafted = 0u;
     int draft[kMaxRows - 1];

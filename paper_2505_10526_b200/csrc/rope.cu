@@ -39,48 +39,56 @@ __device__ __forceinline__ typename RopeVec<V>::T pack(const float (&f)[V]) {
 }
 
 // V: elements per access.  HALF: an item is V pairs, as V elements at i and V at i + rot_dim / 2 (V divides rot_dim / 2), or V elements
-// behind rot_dim that are copied.  Interleaved: an item is 8 elements, of which those below rot_dim turn.
+// behind rot_dim that are copied.  Interleaved: an item is 8 elements, of which those below rot_dim turn.  A thread keeps its place
+// within a head and goes from (token, head) row to row, so there is nothing to divide; the angles' sines and cosines lie in shared memory such
+// that neighbouring places read neighbouring words.
 template <bool HALF, int V>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) {
     using T = typename RopeVec<V>::T;
-    __shared__ float2 s_cs[kRopeMaxTokens][kRopeMaxPairs];
+    constexpr int kPairs = HALF ? V : V / 2;             // pairs of an item
+    __shared__ float2 s_cs[kRopeMaxTokens][kRopeMaxPairs + kPairs];
     const int pairs = p.rot_dim / 2, turning = HALF ? pairs / V : (p.rot_dim + V - 1) / V;
     const int units = turning + (p.copy ? (p.d - (HALF ? p.rot_dim : turning * V)) / V : 0);      // items of a head
     const int heads = p.Hq + p.Hkv;
     const long long n_tokens = (long long)p.B * p.rows, token0 = (long long)blockIdx.x * p.tokens_per_cta;
-    const int n_tok = (int)min((long long)p.tokens_per_cta, n_tokens - token0);
-    const int n_items = n_tok * heads * units;
+    const int n_rows = (int)min((long long)p.tokens_per_cta, n_tokens - token0) * heads;
+    const int step = kRopeThreads / units, first = threadIdx.x / units, unit = threadIdx.x - first * units;      // (units <= 256)
+    const bool turns = unit < turning;
+    const int e = HALF && !turns ? p.rot_dim + (unit - turning) * V : unit * V;                  // the item's first element
     pdl_wait();
     pdl_trigger();
 
-    struct Item { const __nv_bfloat16* src; __nv_bfloat16* dst; int tok, unit; };
-    auto item_at = [&](int idx) {
-        Item it;
-        const int row = idx / units;
-        it.unit = idx - row * units;
-        it.tok = row / heads;
-        const int h = row - it.tok * heads;
-        const long long t = token0 + it.tok;
-        if (h < p.Hq) { it.src = p.q + t * p.q_stride + h * p.d; it.dst = p.q_out + t * p.q_out_stride + h * p.d; }
-        else { it.src = p.k + t * p.k_stride + (h - p.Hq) * p.d; it.dst = p.k_out + t * p.k_out_stride + (h - p.Hq) * p.d; }
-        return it;
+    struct Row { int tok, h; };
+    auto advance = [&](Row& r) {
+        r.h += step;
+        while (r.h >= heads) { r.h -= heads; ++r.tok; }
     };
-    auto first_element = [&](int unit) { return HALF && unit >= turning ? p.rot_dim + (unit - turning) * V : unit * V; };
+    auto source = [&](const Row& r) {
+        const long long t = token0 + r.tok;
+        return (r.h < p.Hq ? p.q + t * p.q_stride + r.h * p.d : p.k + t * p.k_stride + (r.h - p.Hq) * p.d) + e;
+    };
+    auto target = [&](const Row& r) {
+        const long long t = token0 + r.tok;
+        return (r.h < p.Hq ? p.q_out + t * p.q_out_stride + r.h * p.d : p.k_out + t * p.k_out_stride + (r.h - p.Hq) * p.d) + e;
+    };
+    Row row{0, first < step ? first : 0};
+    while (row.h >= heads) { row.h -= heads; ++row.tok; }
     bool have_angles = false;
-    for (int base = 0; base < n_items; base += kRopeThreads * kRopeBatch) {
+    for (int base = first < step ? first : n_rows; base < n_rows || !have_angles; base += step * kRopeBatch) {
         T a[kRopeBatch], b[kRopeBatch];
+        Row at = row;
 #pragma unroll
         for (int k = 0; k < kRopeBatch; ++k) {
-            const int idx = base + k * kRopeThreads + threadIdx.x;
-            if (idx < n_items) {
-                const Item it = item_at(idx);
-                const int e = first_element(it.unit);
-                a[k] = *reinterpret_cast<const T*>(it.src + e);
-                if (HALF && it.unit < turning) b[k] = *reinterpret_cast<const T*>(it.src + e + pairs);
+            if (base + k * step < n_rows) {
+                const __nv_bfloat16* src = source(at);
+                a[k] = *reinterpret_cast<const T*>(src);
+                if (HALF && turns) b[k] = *reinterpret_cast<const T*>(src + pairs);
+                advance(at);
             }
         }
         if (!have_angles) {
             have_angles = true;
+            const int n_tok = n_rows / heads;
             for (int i = threadIdx.x; i < n_tok * pairs; i += kRopeThreads) {
                 const int tok = i / pairs, pair = i - tok * pairs;
                 const long long t = token0 + tok;
@@ -95,18 +103,17 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
                 const long long phase = (long long)((unsigned long long)pos * p.turns[pair]);
                 float sn, cs;
                 sincospif((float)phase * 0x1p-63f, &sn, &cs);             // phase: turns * 2^64
-                s_cs[tok][pair] = make_float2(cs * p.magnitude, (p.backward ? -sn : sn) * p.magnitude);
+                s_cs[tok][pair % kPairs * turning + pair / kPairs] = make_float2(cs * p.magnitude, (p.backward ? -sn : sn) * p.magnitude);
             }
             __syncthreads();
         }
 #pragma unroll
         for (int k = 0; k < kRopeBatch; ++k) {
-            const int idx = base + k * kRopeThreads + threadIdx.x;
-            if (idx >= n_items) continue;
-            const Item it = item_at(idx);
-            const int e = first_element(it.unit);
-            T* dst = reinterpret_cast<T*>(it.dst + e);
-            if (it.unit >= turning) { *dst = a[k]; continue; }
+            if (base + k * step >= n_rows) break;
+            T* dst = reinterpret_cast<T*>(target(row));
+            const float2* cs = s_cs[row.tok] + unit;
+            advance(row);
+            if (!turns) { *dst = a[k]; continue; }
             float x[V];
             unpack<V>(a[k], x);
             if constexpr (HALF) {
@@ -114,16 +121,16 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
                 unpack<V>(b[k], y);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float2 c = s_cs[it.tok][e + i];
+                    const float2 c = cs[i * turning];
                     const float u = x[i] * c.x - y[i] * c.y, w = x[i] * c.y + y[i] * c.x;
                     x[i] = u; y[i] = w;
                 }
-                *reinterpret_cast<T*>(it.dst + e + pairs) = pack<V>(y);
+                *reinterpret_cast<T*>(reinterpret_cast<__nv_bfloat16*>(dst) + pairs) = pack<V>(y);
             } else {
 #pragma unroll
                 for (int i = 0; i < V / 2; ++i) {
                     if (e / 2 + i >= pairs) break;                        // the rest of the group is behind rot_dim
-                    const float2 c = s_cs[it.tok][e / 2 + i];
+                    const float2 c = cs[i * turning];
                     const float u = x[2 * i] * c.x - x[2 * i + 1] * c.y, w = x[2 * i] * c.y + x[2 * i + 1] * c.x;
                     x[2 * i] = u; x[2 * i + 1] = w;
                 }

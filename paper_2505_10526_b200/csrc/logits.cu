@@ -45,10 +45,18 @@ __global__ void __launch_bounds__(kMaxWarps * 32) logit_rules_kernel(const Logit
     const uint32_t prompt = p.prompt_bits && has_word ? p.prompt_bits[(size_t)b * W + word] : 0u;
     const uint32_t output = p.output_bits && has_word ? p.output_bits[(size_t)b * W + word] : 0u;
     int k0 = p.bias_start ? p.bias_start[b] : 0, k1 = p.bias_start ? p.bias_start[b + 1] : 0;
+    // The bits of this lane's groups of four, a nibble each, from a word per lane.
+    auto nibbles = [&](uint32_t words) {
+        uint32_t r = 0u;
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) r |= (__shfl_sync(0xffffffffu, words, k * 4 + lane / 8) >> (lane % 8 * 4) & 15u) << (4 * k);
+        return r;
+    };
+    const uint32_t may = p.allowed ? nibbles(allowed) : 0xffffffffu;
     float x[kVecs][4];
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-        const uint32_t nib = (__shfl_sync(0xffffffffu, allowed, k * 4 + lane / 8) >> (lane % 8 * 4)) & 15u;
+        const uint32_t nib = may >> (4 * k) & 15u;
         const int e0 = k * 128 + lane * 4;
         if constexpr (VEC4) {
             float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
@@ -56,7 +64,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) logit_rules_kernel(const Logit
             x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[k][e] = nib && e0 + e < valid ? z[e0 + e] : -INFINITY;
+            for (int e = 0; e < 4; ++e) x[k][e] = nib >> e & 1u && e0 + e < valid ? z[e0 + e] : -INFINITY;
         }
     }
 
@@ -95,7 +103,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32) logit_rules_kernel(const Logit
             if (d >= 0 && d < p.V && d / 32 == word) drafted |= 1u << (d % 32);
         }
     const uint32_t marked = (prompt | output | biased | drafted) & allowed & (lane * 32 + 32 <= valid ? 0xffffffffu : lane * 32 < valid ? (1u << (valid - lane * 32)) - 1u : 0u);
+    uint32_t changes = 0u;
     if (__any_sync(0xffffffffu, marked != 0u)) {
+        changes = nibbles(marked);
         float rep = p.repetition ? p.repetition[b] : 1.f;
         if (!(rep > 0.f)) rep = 1.f;
         const float freq = p.frequency ? p.frequency[b] : 0.f, pres = p.presence ? p.presence[b] : 0.f;
@@ -138,17 +148,17 @@ __global__ void __launch_bounds__(kMaxWarps * 32) logit_rules_kernel(const Logit
     const bool in_place = p.out == p.logits;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-        const int src = k * 4 + lane / 8, sh = lane % 8 * 4, e0 = k * 128 + lane * 4;
-        const uint32_t m = (__shfl_sync(0xffffffffu, marked, src) >> sh) & 15u, a = (__shfl_sync(0xffffffffu, allowed, src) >> sh) & 15u;
-        if (m) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if ((m >> e) & 1u) x[k][e] = adj[e0 + e];
-        }
+        const int e0 = k * 128 + lane * 4;
+        const uint32_t m = changes >> (4 * k) & 15u, a = may >> (4 * k) & 15u;
         if (a != 15u) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (!((a >> e) & 1u)) x[k][e] = -INFINITY;
+                if (!(a >> e & 1u)) x[k][e] = -INFINITY;
+        }
+        if (m) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (m >> e & 1u) x[k][e] = adj[e0 + e];
         }
         if (out && !(in_place && m == 0u && a == 15u)) {
             if constexpr (VEC4) {
@@ -166,8 +176,11 @@ __global__ void __launch_bounds__(kMaxWarps * 32) logit_rules_kernel(const Logit
         float m = -INFINITY;
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) m = fmaxf(m, fmaxf(fmaxf(x[k][0], x[k][1]), fmaxf(x[k][2], x[k][3])));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        {
+            // (a lane's maximum is no NaN: as a whole number that orders like it, one instruction finds the warp's)
+            const int bits = __float_as_int(m), key = __reduce_max_sync(0xffffffffu, bits < 0 ? bits ^ 0x7fffffff : bits);
+            m = __int_as_float(key < 0 ? key ^ 0x7fffffff : key);
+        }
         float sum = 0.f;
         int idx = 0x7fffffff;
         if (m != -INFINITY) {

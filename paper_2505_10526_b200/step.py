@@ -3,6 +3,12 @@
 ``VerifyStep`` owns the descriptors, the scratch buffers and the output tensors
 for a fixed geometry, so that a step is three C-ABI calls and nothing else.  All
 arithmetic happens inside ``libmassv.so``.
+
+What a serving loop adds around them is switched on per step object: ``rope``
+turns the block's queries and keys first (massv_rotary), ``n_groups`` lets groups of
+sequences share a prefix (massv_verify_attn_shared), ``rules`` puts biases, penalties and
+grammars on the logits and keeps the history they read (massv_accept_logits,
+massv_history_add).
 """
 from __future__ import annotations
 
@@ -18,7 +24,13 @@ STEP_INPUTS = ("q", "k_new", "v_new", "hidden", "draft_tokens", "draft_probs", "
 class VerifyStep:
     def __init__(self, batch, gamma, n_q_heads, n_kv_heads, head_dim, hidden, vocab, temperature,
                  max_pages_per_seq, num_pages, device="cuda", kv_chunk=0, scale=0.0, window=0,
-                 attn_kernel=0, want_logits=False, want_probs=False, want_attn_f32=False):
+                 attn_kernel=0, want_logits=False, want_probs=False, want_attn_f32=False,
+                 rope=None, n_groups=0, rules=False):
+        """``rope``: None, or the keyword arguments of ``rope_desc`` from ``rot_dim`` on together with ``turns``
+        (massv_rope_frequencies); the step's inputs may then hold ``pos_delta`` (int32 [B]).
+        ``n_groups`` > 0: the inputs hold ``group_start`` and ``shared_lens``.
+        ``rules``: the inputs hold ``rules`` (``logit_rules``), and ``run`` adds the emitted tokens to ``output_bits`` and
+        ``counts`` where the inputs hold them."""
         self.device = torch.device(device)
         self.B, self.gamma, self.R = batch, gamma, gamma + 1
         self.T = float(temperature)
@@ -26,8 +38,18 @@ class VerifyStep:
                                   scale=scale, kv_chunk=kv_chunk, window=window, kernel=attn_kernel)
         self.cdesc = mv.accept_desc(batch, gamma, hidden, vocab, temperature)
         dev = self.device
-        self.attn_ws = mv.alloc_workspace(mv.massv_verify_attn_workspace_size(self.adesc), dev)
-        self.accept_ws = mv.alloc_workspace(mv.massv_accept_workspace_size(self.cdesc), dev)
+        self.n_groups, self.rules, self.vocab = n_groups, bool(rules), vocab
+        self.attn_ws = mv.alloc_workspace(mv.massv_verify_attn_shared_workspace_size(self.adesc, n_groups) if n_groups
+                                          else mv.massv_verify_attn_workspace_size(self.adesc), dev)
+        self.accept_ws = mv.alloc_workspace(mv.massv_accept_logits_workspace_size(self.cdesc) if rules
+                                            else mv.massv_accept_workspace_size(self.cdesc), dev)
+        self.rope = None
+        if rope is not None:
+            how = dict(rope)
+            self.turns = how.pop("turns")
+            self.rope = mv.rope_desc(batch, self.R, n_q_heads, n_kv_heads, head_dim, **how)
+            self.q_turned = torch.empty((batch, self.R, n_q_heads, head_dim), dtype=torch.bfloat16, device=dev)
+            self.k_turned = torch.empty((batch, self.R, n_kv_heads, head_dim), dtype=torch.bfloat16, device=dev)
         self.attn_out = torch.empty((batch, self.R, n_q_heads, head_dim), dtype=torch.bfloat16, device=dev)
         self.attn_out_f32 = torch.empty_like(self.attn_out, dtype=torch.float32) if want_attn_f32 else None
         self.lse = torch.empty((batch, self.R, n_q_heads), dtype=torch.float32, device=dev) if want_attn_f32 else None
@@ -35,7 +57,8 @@ class VerifyStep:
         self._out_blob = torch.empty((batch * self.R + batch,), dtype=torch.int32, device=dev)
         self.out_tokens = self._out_blob[:batch * self.R].view(batch, self.R)
         self.accept_len = self._out_blob[batch * self.R:]
-        self.logits = torch.empty((batch, self.R, vocab), dtype=torch.float32, device=dev) if want_logits else None
+        self.logits = torch.empty((batch, self.R, vocab), dtype=torch.float32, device=dev) if want_logits or rules else None
+        self.stats = torch.empty((mv.massv_shard_stats_words(self.cdesc),), dtype=torch.float32, device=dev) if rules else None
         self.probs = (torch.empty((batch, self.R, vocab), dtype=torch.float32, device=dev)
                       if want_probs and temperature > 0 else None)
         self.dev_status = torch.zeros((1,), dtype=torch.int32, device=dev)
@@ -48,14 +71,32 @@ class VerifyStep:
                    cfg.temperature, w["page_table"].shape[1], w["k_pages"].shape[0],
                    device=w["k_pages"].device, **{"window": getattr(cfg, "window", 0), **kw})
 
-    # -- the three calls -------------------------------------------------------------
+    # -- the calls -------------------------------------------------------------------
+    def rotate(self, w):
+        """The block's queries and keys at positions seq_lens + j (+ pos_delta), into the step's own buffers."""
+        mv.massv_rotary(self.rope, self.turns, w["q"], w["k_new"], self.q_turned, self.k_turned, None, w["seq_lens"], w.get("pos_delta"))
+
     def attn(self, w):
-        mv.massv_verify_attn(self.adesc, w["q"], w["k_new"], w["v_new"], w["k_pages"], w["v_pages"],
+        q, k = (self.q_turned, self.k_turned) if self.rope is not None else (w["q"], w["k_new"])
+        if self.n_groups:
+            mv.massv_verify_attn_shared(self.adesc, w["group_start"], w["shared_lens"], q, k, w["v_new"], w["k_pages"], w["v_pages"],
+                                        w["page_table"], w["seq_lens"], self.attn_out, self.attn_out_f32, self.lse,
+                                        self.attn_ws, self.dev_status)
+            return
+        mv.massv_verify_attn(self.adesc, q, k, w["v_new"], w["k_pages"], w["v_pages"],
                              w["page_table"], w["seq_lens"], self.attn_out, self.attn_out_f32, self.lse,
                              self.attn_ws, self.dev_status)
 
     def accept(self, w):
         sampling = self.T > 0
+        if self.rules:
+            # the logits of all rows, then the rules over them in place with the acceptance behind
+            mv.massv_shard_lm_head(self.cdesc, 1, 0, w["hidden"], w["lm_head"], self.logits, self.stats, self.dev_status)
+            mv.massv_accept_logits(self.cdesc, w["rules"], self.logits, self.logits, w["draft_tokens"],
+                                   w.get("draft_probs") if sampling else None, w.get("u_accept") if sampling else None,
+                                   w.get("u_sample") if sampling else None, self.out_tokens, self.accept_len,
+                                   self.probs, self.accept_ws, self.dev_status)
+            return
         mv.massv_accept(self.cdesc, w["hidden"], w["lm_head"], w["draft_tokens"],
                         w.get("draft_probs") if sampling else None, w.get("u_accept") if sampling else None,
                         w.get("u_sample") if sampling else None, self.out_tokens, self.accept_len,
@@ -64,12 +105,20 @@ class VerifyStep:
     def commit(self, seq_lens, rollback=False):
         mv.massv_kv_commit(self.B, self.gamma, None if rollback else self.accept_len, seq_lens, self.dev_status)
 
+    def record(self, w):
+        """The step's emitted tokens into the history that the rules read."""
+        mv.massv_history_add(self.vocab, self.out_tokens, self.accept_len, w["output_bits"], w.get("counts"), self.dev_status)
+
     def run(self, w, commit=True):
         """Enqueue one whole step on the current stream (no synchronisation)."""
+        if self.rope is not None:
+            self.rotate(w)
         self.attn(w)
         self.accept(w)
         if commit:
             self.commit(w["seq_lens"])
+            if self.rules and w.get("output_bits") is not None:
+                self.record(w)
 
     # -- end-to-end step with host buffers ----------------------------------------------
     def host_inputs_like(self, tensors):

@@ -13,13 +13,16 @@
 //
 // PREFIX items: a tile is as many whole (sequence, block row) pairs of a KV head's G query heads as fit 128 rows.  At head_dim 64 and
 // 128 a CTA works on two tiles at once, so that one tile's products run under the other's exponentials; both share each K and V
-// block.  At 256 the accumulator leaves room for one, whose scores are double buffered instead.  Every position is seen by every row.
+// block; each tile's products are issued by a warp of its own, 64 positions at a time, so that a tile's next scores are made while its
+// softmax is at the other half.  At 256 the accumulator leaves room for one, whose scores are double buffered instead.  Every position is
+// seen by every row.
 // TAIL items: the positions of one sequence behind the prefix, block rows included (appended here), for its G * R <= 64 rows.  The
 // blocks of all tails of a CTA form one pipeline across items (the next item's queries have a buffer of their own): the scores run two
 // blocks ahead of the weights, and where there is room for two accumulators the blocks alternate between them.
 //
-// Warps 0 and 3 copy K and V (TMA), each into a ring of its own; warp 1 issues the products; warp 2 and the last warp patch the block's own
-// K and V rows into the blocks that hold their positions and store them to their page slots; four warps per tile make the softmax.
+// Warps 0 and 3 copy K and V (TMA), each into a ring of its own; warp 1 issues the products, for a second tile warp 2 does, which in tails
+// patches the block's own K rows into the blocks that hold their positions and stores them to their page slots, as the last warp does
+// with V's; four warps per tile make the softmax.
 //
 // All items form one line, a block costing what its kind costs (below), cut into equal ranges for a persistent grid of one CTA per
 // SM: prefix items, which the tensor cores bound, and tails, which memory bounds, are at work at the same time.  What a CTA has
@@ -36,8 +39,10 @@ constexpr int kTileRows = 128;
 constexpr int kPagesPerBlock = kPrefixBlock / kPageSize;
 constexpr float kRescaleThreshold = 8.f;   // log2 units a row's maximum may outgrow its reference by
 
-// Cost of a block: products of two tiles, of one, of a tail; and what an item costs beside its blocks (queries, write-out).
-constexpr int kCostTwo = 8, kCostOne = 7, kCostTail = 7, kCostPrefixItem = 8, kCostTailItem = 5;
+// Cost of a block: products of two tiles, of one, of a tail; and what an item costs beside its blocks (queries, write-out).  Set by
+// measurement: equal ranges should take equal time (64 sequences of 28 heads of 128 in three groups, prefixes up
+// to 16,384: 129 us, with 7 for two tiles and 8 for a tail 137; 31 of 16 heads of 256, two groups up to 4,111: 62 us, with 7 for one tile 64).
+constexpr int kCostTwo = 8, kCostOne = 6, kCostTail = 7, kCostPrefixItem = 8, kCostTailItem = 5;
 constexpr int kCostMost = kCostTwo + kCostPrefixItem;
 
 // Blocks of an item that begins at `start`: block 0 there, block k > 0 at start + item + k * block.  The first block that begins at or
@@ -166,7 +171,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __shared__ __align__(8) uint64_t ready_bar[2 * E], empty_bar[2 * E];
     __shared__ __align__(8) uint64_t landed_bar[2 * E];                // the bytes of an entry that still needs patching
     __shared__ __align__(8) uint64_t q_ready_bar[2], q_free_bar[2];   // by query buffer: a prefix item has both, tails take turns
-    __shared__ __align__(8) uint64_t s_full_bar[2], p_full_bar[2][2];  // by score buffer; weights of the first and the second 64 positions
+    __shared__ __align__(8) uint64_t s_full_bar[2][2], p_full_bar[2][2];      // by score buffer; of the first and the second 64 positions
     __shared__ __align__(8) uint64_t o_full_bar[2], o_free_bar[2];     // by tile
     __shared__ __align__(8) uint64_t pv_done_bar;                      // one tile: O is up to date
     __shared__ __align__(8) uint64_t pv_half_bar[2];                   // by accumulator: it has the first 64 positions of a block
@@ -181,7 +186,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     // barriers, one thread each (45 initialisations by one thread take 1,100 cycles)
     {
         struct { uint64_t* bar; int n, arrivals; } const kinds[] = {
-            {ready_bar, 2 * E, 1}, {empty_bar, 2 * E, 1}, {landed_bar, 2 * E, 1}, {q_ready_bar, 2, 1}, {q_free_bar, 2, 1}, {s_full_bar, 2, 1}, {&p_full_bar[0][0], 4, 4},
+            {ready_bar, 2 * E, 1}, {empty_bar, 2 * E, NT}, {landed_bar, 2 * E, 1}, {q_ready_bar, 2, 1}, {q_free_bar, 2, NT}, {&s_full_bar[0][0], 4, 1}, {&p_full_bar[0][0], 4, 4},
             {o_full_bar, 2, 1}, {o_free_bar, 2, 4}, {&pv_done_bar, 1, 1}, {pv_half_bar, 2, 1}, {run_ready_bar, kRunQueue, 1},
             {run_free_bar, kRunQueue, 4 + 4 * NT}};                   // V, two helpers, products, softmax
         int at = threadIdx.x;
@@ -347,8 +352,6 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         r.n = 0;
         return false;
     };
-    // Two tiles on one prefix; everything else is one pipeline over all blocks, in which the scores run two blocks ahead.
-    auto paired = [&](const Run& r) { return NT == 2 && !r.tail; };
 
     constexpr uint32_t tmem_base = 0;                                  // all 512 columns are this CTA's: they begin at 0
     volatile int* abort_ptr = &abort_flag;
@@ -361,6 +364,82 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         if (!keep && lane == 0) mbar_arrive(&run_free_bar[i % kRunQueue]);
         return r.n > 0;
     };
+
+    // ------------------------------------------------ products of prefix items on two tiles: warp 1 issues the first tile's, warp 2 the second's
+    // (A wait takes 200 cycles in these warps even where there is nothing to wait for, since the products keep shared memory busy: one warp for
+    // both tiles is at it all the time and no faster.)  The whole warp runs this code, so that addresses and descriptors stay warp-uniform;
+    // one elected lane issues.
+    const uint32_t lead = elect_one();
+    const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem)), k_lo0 = umma_desc_lo(smem_u32(ring_smem));
+    const uint32_t v_lo0 = (((smem_u32(ring_smem) + E * Cfg::kEntry) & 0x3FFFFu) >> 4) | ((uint32_t)((kPrefixBlock / PARTS * 128) >> 4) << 16);
+    constexpr uint32_t idesc_pv = umma_idesc_bf16(kTileRows, D, true);
+    Run pr;
+    int p_run = 0, p_blk = 0, p_two = 0, p_blk_two = 0;                // prefix items so far, their blocks; of these on two tiles
+    bool p_any = false;
+    if (warp == 1 || (NT == 2 && warp == 2)) p_any = take_run(0, pr, true);
+    if constexpr (NT == 2) {
+        if (warp == 1 || warp == 2) {
+            const int x = warp - 1;
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, uint32_t parity) { if (!mbar_wait_warp(bar, parity, abort_ptr)) ok = false; };
+            for (; ok && p_any && !pr.tail; p_any = take_run(++p_run, pr, true)) {
+                if (lane == 0) mbar_arrive(&run_free_bar[p_run % kRunQueue]);
+                const int n = pr.n, tau = x ? p_blk_two : p_blk, use = x ? p_two : p_run;
+                const bool two = pr.n_rows[1] > 0;
+                // alone, a warp gives back for both
+                auto give = [&](uint64_t* bar) { umma_commit_lead(lead, bar); if (!two && lane == 0) mbar_arrive(bar); };
+                if (x == 0 || two) {
+                    wait(&q_ready_bar[0], (uint32_t)p_run & 1u);
+                    for (int t = -1; t < n && ok; ++t) {
+                        // 64 positions at a time: the weights of block t times V, then, over what they left, the scores of block t + 1.  So the
+                        // scores that a tile's softmax takes next are made while it is at the other half.
+                        const int kb = p_blk + t + 1, vb = p_blk + t;
+                        // (the three in one: their latencies overlap)
+                        if (t == 0) wait(&o_free_bar[x], (uint32_t)(use & 1) ^ 1u);
+                        uint64_t *const k_ready = &ready_bar[kb % E], *const v_ready = &ready_bar[E + vb % E];
+                        const uint32_t k_lap = (uint32_t)(kb / E) & 1u, v_lap = (uint32_t)(vb / E) & 1u, p_lap = (uint32_t)(tau + t) & 1u;
+                        if (t < 0) wait(k_ready, k_lap);
+                        else if (!mbar_wait_warp3(v_ready, v_lap, t + 1 < n ? k_ready : v_ready, t + 1 < n ? k_lap : v_lap, &p_full_bar[x][0], p_lap, abort_ptr)) ok = false;
+                        const uint32_t k_lo = k_lo0 + (uint32_t)(kb % E * (Cfg::kEntry >> 4)), v_lo = v_lo0 + (uint32_t)(vb % E * (Cfg::kEntry >> 4));
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const uint32_t s_tmem = tmem_base + (uint32_t)(x * kPrefixBlock + half * (kPrefixBlock / 2));
+                            if (t >= 0) {
+                                if (half == 1) wait(&p_full_bar[x][1], p_lap);
+                                if (!ok) break;
+                                tc_fence_after();
+#pragma unroll
+                                for (int ks = 0; ks < kPrefixBlock / 32; ++ks)
+                                    umma_bf16_ts_lead(lead, tmem_base + Cfg::kTmemO + (uint32_t)(x * D), s_tmem + (uint32_t)(ks * 8),
+                                                      v_lo + (uint32_t)((half * (kPrefixBlock / 2 * 128) + ks * 2048) >> 4), idesc_pv, t == 0 && half == 0 && ks == 0 ? 0u : 1u);
+                                if (half == 0) umma_commit_lead(lead, &pv_half_bar[x]);
+                            }
+                            if (!ok) break;
+                            if (t + 1 < n) {
+                                tc_fence_after();
+#pragma unroll
+                                for (int kk = 0; kk < D / 16; ++kk)
+                                    umma_bf16_lead(lead, s_tmem, q_lo + (uint32_t)((x * Cfg::kQTile + (kk >> 2) * (kTileRows * 128) + (kk & 3) * 32) >> 4),
+                                                   k_lo + (uint32_t)((half * (kPrefixBlock / 2 * 128) + (kk >> 2) * (kPrefixBlock * 128) + (kk & 3) * 32) >> 4),
+                                                   umma_idesc_bf16(kTileRows, kPrefixBlock / 2, false), kk == 0 ? 0u : 1u);
+                                umma_commit_lead(lead, &s_full_bar[x][half]);
+                            } else if (half == 1) {
+                                umma_commit_lead(lead, &o_full_bar[x]);
+                            }
+                        }
+                        if (!ok) break;
+                        if (t >= 0) give(&empty_bar[E + vb % E]);
+                        if (t + 1 < n) give(&empty_bar[kb % E]);
+                        if (t + 2 == n) give(&q_free_bar[0]);
+                    }
+                }
+                p_blk += n;
+                if (two) { p_blk_two += n; ++p_two; }
+            }
+            if (!ok) p_any = false;
+        }
+    }
+
     if (warp == 0 || warp == 3) {
         // ------------------------------------------------ copies: K (and the queries) by warp 0, V by warp 3
         const bool is_v = warp == 3;
@@ -439,7 +518,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         // ------------------------------------------------ helpers: the block's own rows, and what lies behind the last position
         const bool is_v = warp != 2;
         uint32_t landed_phase = 0;       // bit e: parity of the next completion of landed_bar[e]
-        int it = 0;                      // entries of the ring so far
+        int it = p_blk;                  // entries of the ring so far (the K warp comes from the prefix items)
         bool ok = true;
         // Block t of a run, entry by entry.
         auto patch = [&](const Run& r, int t) {
@@ -494,24 +573,23 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 if (lane == 0) mbar_arrive(&ready_bar[e]);
             }
         };
-        Run r;
-        for (int run = 0; ok && take_run(run, r, false); ++run) {
+        Run r = pr;
+        int run = p_run;
+        if (is_v || NT == 1) p_any = take_run(0, r, true);
+        for (; ok && p_any; p_any = take_run(++run, r, true)) {
+            if (lane == 0) mbar_arrive(&run_free_bar[run % kRunQueue]);
             const int t0 = r.tail ? min(r.n, max(0, r.L - r.pos0) / kPrefixBlock) : r.n;       // the first block with a position not in the cache
             it += t0 * PARTS;
             for (int t = t0; t < r.n && ok; ++t) patch(r, t);
         }
     } else if (warp == 1) {
-        // ------------------------------------------------ products
-        // The whole warp runs this code, so that addresses and descriptors stay warp-uniform; one elected lane issues.
+        // ------------------------------------------------ products of everything else: one pipeline over all blocks
         constexpr uint32_t idesc_qk = umma_idesc_bf16(kTileRows, kPrefixBlock, false);
-        constexpr uint32_t idesc_pv = umma_idesc_bf16(kTileRows, D, true);
-        constexpr int kVRegion = kPrefixBlock / PARTS * 128;
-        const uint32_t lead = elect_one();
-        const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem)), k_lo0 = umma_desc_lo(smem_u32(ring_smem));
-        const uint32_t v_lo0 = (((smem_u32(ring_smem) + E * Cfg::kEntry) & 0x3FFFFu) >> 4) | ((uint32_t)(kVRegion >> 4) << 16);
         bool ok = true;
-        int ek = 0, ev = 0;                                            // ring entries
-        uint32_t lap_k = 0, lap_v = 0, s_lap[2] = {0, 0}, q_lap[2] = {0, 0}, o_lap[2] = {1, 1};       // parities of the next waits
+        int ek = p_blk % E, ev = ek;                                   // ring entries
+        // parities of the next waits
+        uint32_t lap_k = (uint32_t)(p_blk / E) & 1u, lap_v = lap_k, s_lap[2] = {(uint32_t)p_blk & 1u, (uint32_t)p_blk_two & 1u}, q_lap[2] = {NT == 2 ? (uint32_t)p_run & 1u : 0u, 0u},
+                 o_lap[2] = {(uint32_t)(p_run & 1) ^ 1u, (uint32_t)(p_two & 1) ^ 1u};
         auto wait = [&](uint64_t* bar, uint32_t parity) { if (!mbar_wait_warp(bar, parity, abort_ptr)) ok = false; };
         // S[buf] = Q K^T over `part`'s share of d; the queries q_off bytes into their place
         auto qk = [&](uint32_t q_off, int buf, int part) {
@@ -528,59 +606,20 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         auto pv = [&](int x, int buf, int half, bool first) {
             tc_fence_after();
             const uint32_t v_lo = v_lo0 + (uint32_t)(ev * (Cfg::kEntry >> 4) + (PARTS == 1 ? half * (kPrefixBlock / 2 * 128 >> 4) : 0));
-            const uint32_t d_tmem = tmem_base + Cfg::kTmemO + (uint32_t)(x * D), a0 = tmem_base + (uint32_t)(buf * kPrefixBlock + half * (kPrefixBlock / 4));
+            const uint32_t d_tmem = tmem_base + Cfg::kTmemO + (uint32_t)(x * D), a0 = tmem_base + (uint32_t)(buf * kPrefixBlock + half * (kPrefixBlock / 2));
 #pragma unroll
             for (int ks = 0; ks < kPrefixBlock / 32; ++ks)
                 umma_bf16_ts_lead(lead, d_tmem, a0 + (uint32_t)(ks * 8), v_lo + (uint32_t)((ks * 2048) >> 4), idesc_pv, ks == 0 && first ? 0u : 1u);
         };
-        auto k_done = [&]() { umma_commit_lead(lead, &empty_bar[ek]); if (++ek == E) { ek = 0; lap_k ^= 1u; } };
-        auto v_done = [&]() { umma_commit_lead(lead, &empty_bar[E + ev]); if (++ev == E) { ev = 0; lap_v ^= 1u; } };
+        auto give = [&](uint64_t* bar) { umma_commit_lead(lead, bar); if (NT == 2 && lane == 0) mbar_arrive(bar); };      // (for both issuers)
+        auto k_done = [&]() { give(&empty_bar[ek]); if (++ek == E) { ek = 0; lap_k ^= 1u; } };
+        auto v_done = [&]() { give(&empty_bar[E + ev]); if (++ev == E) { ev = 0; lap_v ^= 1u; } };
         // (blocks of the scores and of the products: run, block within, blocks of the run)
-        Run kr, vr;
-        int k_run = 0, k_t = 0, v_run, v_t = 0;
-        bool any = take_run(0, kr, true);
-        if constexpr (NT == 2) {
-            for (; ok && any && paired(kr); any = take_run(k_run, kr, true)) {
-                if (lane == 0) mbar_arrive(&run_free_bar[k_run % kRunQueue]);
-                ++k_run;
-                const int n = kr.n;
-                const bool two = kr.n_rows[1] > 0;
-                wait(&q_ready_bar[0], q_lap[0]); q_lap[0] ^= 1u;
-                for (int t = -1; t < n && ok; ++t) {
-                    // the weights of block t times V, then, over each tile's P, the scores of block t + 1
-                    if (t >= 0) wait(&ready_bar[E + ev], lap_v);
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (x == 1 && !two) break;
-                        if (t >= 0) {
-                            if (t == 0) { wait(&o_free_bar[x], o_lap[x]); o_lap[x] ^= 1u; }
-                            wait(&p_full_bar[x][0], s_lap[x]);
-                            if (!ok) break;
-                            pv(x, x, 0, t == 0);
-                            umma_commit_lead(lead, &pv_half_bar[x]);
-                            wait(&p_full_bar[x][1], s_lap[x]); s_lap[x] ^= 1u;
-                            if (!ok) break;
-                            pv(x, x, 1, false);
-                        }
-                        if (t + 1 < n) {
-                            if (x == 0) { wait(&ready_bar[ek], lap_k); if (!ok) break; }
-                            qk((uint32_t)(x * Cfg::kQTile), x, 0);
-                            umma_commit_lead(lead, &s_full_bar[x]);
-                        } else {
-                            umma_commit_lead(lead, &o_full_bar[x]);
-                        }
-                    }
-                    if (!ok) break;
-                    if (t >= 0) v_done();
-                    if (t + 1 < n) k_done();
-                    if (t + 2 == n) umma_commit_lead(lead, &q_free_bar[0]);
-                }
-            }
-        }
-        // The pipeline: a block's scores go over the P of two blocks before, behind the product that read it.
-        vr = kr;
-        v_run = k_run;
-        bool have_v = any && ok;
+        // A block's scores go over the P of two blocks before, behind the product that read it.
+        Run kr = pr, vr = pr;
+        int k_run = p_run, k_t = 0, v_run = p_run, v_t = 0;
+        bool any = p_any, have_v = any;
+        if (any && p_two > 0) wait(&o_full_bar[1], (uint32_t)(p_two - 1) & 1u);       // the second tile's products are another warp's
         int turn = 0, n_s = 0, n_p = 0;                               // tails so far (scores), blocks so far
         while (have_v && ok) {
             if (any && n_s < n_p + 2) {
@@ -594,9 +633,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     k_done();
                 }
                 if (!ok) break;
-                umma_commit_lead(lead, &s_full_bar[buf]);
+                umma_commit_lead(lead, &s_full_bar[buf][0]);
                 if (++k_t == kr.n) {
-                    umma_commit_lead(lead, &q_free_bar[qb]);
+                    give(&q_free_bar[qb]);
                     if (kr.tail) ++turn;
                     any = take_run(++k_run, kr, true);
                     k_t = 0;
@@ -637,6 +676,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         int at = 0;                                                    // blocks of the pipeline ahead of this run
         Run r;
         for (int run = 0; ok && take_run(run, r, false); ++run) {
+            const bool halves = NT == 2 && !r.tail;                    // the scores come 64 positions at a time
             const bool alone = r.tail && NT == 2;                      // every second block is this accumulator's
             const int turn = alone ? (at & 1) ^ x : x;                 // its first block; the place of its piece
             if (alone) at += r.n;
@@ -647,7 +687,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             for (int t = alone ? turn : 0; t < r.n && ok; t += alone ? 2 : 1, ++tau) {
                 const int buf = NT == 2 ? x : tau & 1;
                 const uint32_t parity = (uint32_t)(NT == 2 ? tau : tau >> 1) & 1u;
-                if (!mbar_wait_warp(&s_full_bar[buf], parity, abort_ptr)) { ok = false; break; }
+                if (NT == 1 && !mbar_wait_warp(&s_full_bar[buf][0], parity, abort_ptr)) { ok = false; break; }
                 tc_fence_after();
                 if (some) {
                     const uint32_t tmem_s = tmem_base + lane_base + (uint32_t)(buf * kPrefixBlock);
@@ -659,6 +699,10 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     // long (a CTA waits for its first blocks' instructions one by one).
 #pragma unroll 1
                     for (int h = 0; h < 2; ++h) {
+                        if (NT == 2 && (h == 0 || halves)) {
+                            if (!mbar_wait_warp(&s_full_bar[buf][h], parity, abort_ptr)) { ok = false; break; }
+                            tc_fence_after();
+                        }
                         uint32_t s[64];
                         tmem_ld_row32(tmem_s + (uint32_t)(h * 64), s);
                         tmem_ld_row32(tmem_s + (uint32_t)(h * 64 + 32), s + 32);
@@ -677,10 +721,11 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             const float factor = moved && ref != -INFINITY ? exp2f(ref - mx) : 1.f;
                             ref = moved ? mx : ref;
                             if (__any_sync(0xffffffffu, factor != 1.f)) {
-                                // O has to be up to date: with the block's first half where this is its second, else with the block before (two
-                                // accumulators: this block's scores stand behind it)
+                                // O has to be up to date: with the block's first half where this is its second, else with the block before (scores
+                                // in halves: those of this block's second half stand behind it; a tail with two accumulators: this block's do)
                                 if (h == 1 && !mbar_wait_warp(&pv_half_bar[x], (uint32_t)tau & 1u, abort_ptr)) ok = false;
                                 if (h == 0 && NT == 1 && !mbar_wait_warp(&pv_done_bar, (uint32_t)(tau - 1) & 1u, abort_ptr)) ok = false;
+                                if (h == 0 && halves && !mbar_wait_warp(&s_full_bar[x][1], parity, abort_ptr)) ok = false;
                                 if (!ok) break;
                                 tc_fence_after();
 #pragma unroll 1
@@ -710,7 +755,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                                 part[c & 3] = add2(part[c & 3], pack2(p0, p1));
                                 pk[c] = bf16x2(p0, p1);
                             }
-                            tmem_st_row16(tmem_s + (uint32_t)(h * 32 + c0 / 2), pk);       // (over columns that have been read: P is half as wide as S)
+                            tmem_st_row16(tmem_s + (uint32_t)(h * 64 + c0 / 2), pk);       // (over columns that have been read: P is half as wide as S)
                         }
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                         tc_fence_before();
@@ -721,8 +766,12 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     const float2 sum = unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])));
                     l_run += sum.x + sum.y;
                 } else {
-                    tc_fence_before();
-                    if (lane == 0) { mbar_arrive(&p_full_bar[buf][0]); mbar_arrive(&p_full_bar[buf][1]); }
+                    for (int h = 0; h < 2; ++h) {
+                        if (NT == 2 && (h == 0 || halves) && !mbar_wait_warp(&s_full_bar[buf][h], parity, abort_ptr)) { ok = false; break; }
+                        tc_fence_after();
+                        tc_fence_before();
+                        if (lane == 0) mbar_arrive(&p_full_bar[buf][h]);
+                    }
                 }
             }
             if (!ok || !mbar_wait_warp(&o_full_bar[x], (uint32_t)uses & 1u, abort_ptr)) { ok = false; break; }

@@ -51,6 +51,29 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, v
     return __all_sync(0xffffffffu, ok);
 }
 
+// For three barriers at once: the polls' latencies overlap (shared memory that matrix products keep busy answers one in 200 cycles).
+__device__ __forceinline__ bool mbar_wait_warp3(uint64_t* bar0, uint32_t parity0, uint64_t* bar1, uint32_t parity1, uint64_t* bar2, uint32_t parity2,
+                                                volatile int* abort_flag) {
+    bool ok = false;
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+        uint32_t all;
+        asm volatile(
+            "{\n\t.reg .pred p, q, r;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 r, [%5], %6;\n\t"
+            "and.pred p, p, q;\n\tand.pred p, p, r;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(all)
+            : "r"(smem_u32(bar0)), "r"(parity0), "r"(smem_u32(bar1)), "r"(parity1), "r"(smem_u32(bar2)), "r"(parity2)
+            : "memory");
+        if (all) { ok = true; break; }
+        if ((i & 255u) == 255u && *abort_flag) break;
+    }
+    if (!ok) *abort_flag = 1;
+    return __all_sync(0xffffffffu, ok);
+}
+
 __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar, uint64_t policy) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"

@@ -649,8 +649,10 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             if (first) { wait(&o_free_bar[x], x ? o_lap[1] : o_lap[0]); if (x) o_lap[1] ^= 1u; else o_lap[0] ^= 1u; }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                if (half == 0 || PARTS == 2) wait(&ready_bar[E + ev], lap_v);
-                wait(&p_full_bar[buf][half], lap);
+                // (a wait for both halves of the weights would be one for ever: the second may wait for the first's product)
+                uint64_t* const p_bar = &p_full_bar[buf][half];
+                if (half == 0 || PARTS == 2) { if (!mbar_wait_warp3(p_bar, lap, &ready_bar[E + ev], lap_v, p_bar, lap, abort_ptr)) ok = false; }
+                else wait(p_bar, lap);
                 if (!ok) break;
                 pv(x, buf, half, first && half == 0);
                 if (half == 0) umma_commit_lead(lead, &pv_half_bar[x]);

@@ -27,6 +27,11 @@
 // All items form one line, a block costing what its kind costs (below), cut into equal ranges for a persistent grid of one CTA per
 // SM: prefix items, which the tensor cores bound, and tails, which memory bounds, are at work at the same time.  What a CTA has
 // of an item is a piece (O, m, l); attn_shared_merge_kernel adds the pieces of every row up, in order.
+//
+// What bounds it: a two-tile block is 2,048 cycles of products (64 for each 128 x 128 x 16; 48 instead of 32 for one of 64 scores,
+// whose operands shared memory cannot deliver faster) and 2,048 of exponentials, and takes about 3,300: products,
+// copies and tensor-memory traffic share one shared memory.  A prefix alone (64 sequences of 6 rows, 28 heads of 128, 16,384
+// positions) runs at 770 TFLOP/s, tails alone (64 of 1,000 positions, 16 heads of 256) at 5.3 TB/s of K and V.
 #include "kernels.cuh"
 #include "ptx.cuh"
 #include "umma.cuh"
@@ -817,7 +822,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 
 // Pieces of a row added up.  A unit is eight columns of one query row of a (sequence, KV head) pair, rows side by side.  A thread goes through
 // its unit's pieces four at a time, all their loads in flight together, with a running maximum; where there are few units, eight threads
-// share one, each taking every eighth four.  The order of the sums is fixed.
+// share one, each taking every eighth four: few units means that one prefix is cut into many pieces (whole calls, one thread to a unit against
+// eight: 2 sequences behind 16,384 positions 30.3 and 22.1 us; 8 behind 2,048 25.0 and 27.5, 16 behind 2,304 28.6 and 35.4, 64 behind three long prefixes
+// 128 and 170).  The order of the sums is fixed.
 template <int SHARE>
 __global__ void __launch_bounds__(SHARE == 1 ? 128 : 256) attn_shared_merge_kernel(const SharedAttnParams p) {
     constexpr int kUnits = SHARE == 1 ? 128 : 256 / SHARE;             // of a CTA
@@ -943,6 +950,7 @@ cudaError_t launch(const SharedAttnParams& p, cudaStream_t stream) {
     e = launch_pdl(attn_shared_kernel<D>, dim3(ctas), dim3(Cfg::kThreads), smem, stream, mk, mv, mq, mqt, p);
     if (e != cudaSuccess) return e;
     const int pairs = p.a.B * p.a.Hkv, units = G * p.a.R * (D / 8);
+    // eight threads to a unit as long as that gives every SM no more than 512 threads
     if ((long)pairs * units * 8 > 512L * ctas) return launch_pdl(attn_shared_merge_kernel<1>, dim3(pairs, (units + 127) / 128), dim3(128), 0, stream, p);
     return launch_pdl(attn_shared_merge_kernel<8>, dim3(pairs, (units + 31) / 32), dim3(256), 0, stream, p);
 }

@@ -4,7 +4,8 @@
 // pair group) turns with them, so the angle of a pair is computed once however many heads share it.  The angle is exact: turns per
 // position are a 64-bit fraction, and position * fraction wraps modulo 2^64 exactly where the angle wraps modulo one turn, so
 // the upper bits are the angle in [-1/2, 1/2) turns whatever the position.  The heads' elements are requested ahead of that, so that
-// the arithmetic of the angles runs under the loads.
+// the arithmetic of the angles runs under the loads.  HBM bounds it: one read and one write of the heads, 8,191 tokens of 28 + 4 heads
+// of 128 24 us (5.5 TB/s), 32,768 97 us; a block of six tokens is a launch, 2.9 us.
 #include <math.h>
 
 #include "kernels.cuh"
@@ -152,7 +153,8 @@ cudaError_t launch(const RopeParams& p, int grid, cudaStream_t stream) {
 cudaError_t launch_rope(const RopeParams& in, cudaStream_t stream) {
     RopeParams p = in;
     const long long tokens = (long long)p.B * p.rows;
-    // several tokens to a CTA once there are enough of them to fill the machine
+    // several tokens to a CTA once there are enough of them to fill the machine (28 + 4 heads of 128, one token to a CTA against four: 300
+    // tokens 4.45 and 4.51 us, 1,184 5.1 and 4.7, 2,400 9.1 and 7.5, 8,191 31.1 and 23.3)
     p.tokens_per_cta = tokens >= 8LL * device_sm_count() ? kRopeMaxTokens : 1;
     const int grid = (int)((tokens + p.tokens_per_cta - 1) / p.tokens_per_cta);
     const int half = p.rot_dim / 2;

@@ -116,6 +116,35 @@ def test_accept_workspace_of_exactly_the_size(mv):
     assert int(status.item()) == 0 and bool((big[n:] == 0x5a).all()) and int(lens.min()) >= 1
 
 
+@pytest.mark.parametrize("T", [0.0, 1.0])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_accept_with_logits_that_are_no_numbers(mv, T, value):
+    """A row of nothing but NaN (or, at T > 0, one with an infinite logit) under no mask: reported, tokens inside the vocabulary, the others served as without it."""
+    batch, gamma, vocab = 3, 1, 3000
+    s = rules_of._make(batch, gamma, vocab, ("history",), 10)
+    desc = mv.accept_desc(batch, gamma, 64, vocab, T)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.softmax(torch.randn((batch, gamma, vocab), device="cuda", generator=g), -1)
+    u, v = torch.rand((batch, gamma), device="cuda", generator=g), torch.rand((batch, gamma + 1), device="cuda", generator=g)
+
+    def call(z):
+        tokens, lens, status = torch.zeros((batch, gamma + 1), dtype=torch.int32, device="cuda"), torch.zeros((batch,), dtype=torch.int32, device="cuda"), torch.zeros((1,), dtype=torch.int32, device="cuda")
+        ws = mv.alloc_workspace(mv.massv_accept_logits_workspace_size(desc), "cuda")
+        mv.massv_accept_logits(desc, rules_of._rules(mv, s), z, torch.empty_like(z), s["draft_tokens"], q if T else None, u if T else None, v if T else None, tokens, lens, None, ws, status)
+        return tokens, lens, int(status.item())
+    tokens, lens, status = call(s["logits"])
+    z = s["logits"].clone()
+    if value != value:
+        z[1] = value
+    else:
+        z[1, 0, 5] = value
+    bad_tokens, bad_lens, bad_status = call(z)
+    assert status == 0 and (bad_status == -1 or (T == 0 and value == float("inf")))
+    assert int(bad_lens.min()) >= 1 and int(bad_lens.max()) <= gamma + 1 and all(0 <= int(bad_tokens[1, i]) < vocab for i in range(int(bad_lens[1])))
+    for b in (0, 2):
+        assert torch.equal(tokens[b], bad_tokens[b]) and int(lens[b]) == int(bad_lens[b])
+
+
 def test_the_build_that_checks_its_indices():
     here = os.path.dirname(os.path.abspath(__file__))
     files = [os.path.join(here, f) for f in ("test_attn_shared.py", "test_rotary.py", "test_logit_rules.py")]

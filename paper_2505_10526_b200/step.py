@@ -39,6 +39,8 @@ class VerifyStep:
         self.cdesc = mv.accept_desc(batch, gamma, hidden, vocab, temperature)
         dev = self.device
         self.n_groups, self.rules, self.vocab = n_groups, bool(rules), vocab
+        if n_groups and mv.massv_verify_attn_shared_workspace_size(self.adesc, n_groups) == 0:
+            raise ValueError("massv: groups that share a prefix take no window, at most 256 groups and 2,048 sequences")
         self.attn_ws = mv.alloc_workspace(mv.massv_verify_attn_shared_workspace_size(self.adesc, n_groups) if n_groups
                                           else mv.massv_verify_attn_workspace_size(self.adesc), dev)
         self.accept_ws = mv.alloc_workspace(mv.massv_accept_logits_workspace_size(self.cdesc) if rules

@@ -34,6 +34,13 @@ def test_refusals(mv):
         mv.massv_verify_attn_shared(mv.accept_desc(1, 1, 64, 64, 1.0), i, i[:1], b, b, b, b, b, i, i, b)
 
 
+@pytest.mark.parametrize("kw", [dict(window=64, n_groups=1), dict(n_groups=257), dict(n_groups=-1)])
+def test_a_step_that_cannot_share_is_refused(mv, kw):
+    import paper_2505_10526_b200 as pkg
+    with pytest.raises(ValueError, match="share a prefix"):
+        pkg.VerifyStep(4, 3, 8, 2, 64, 64, 64, 0.0, 20, 100, device="cpu", **kw)
+
+
 # ---------------------------------------------------------------- on the GPU
 def _make(sizes, shared, tails, gamma, hq, hkv, d, seed, slope=0.0, extra_pages=1):
     """Groups of sizes[g] sequences whose page tables agree on the whole pages of shared[g] positions; tails: positions behind them."""

@@ -391,9 +391,20 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 if (lane == 0) mbar_arrive(&run_free_bar[p_run % kRunQueue]);
                 const int n = pr.n, tau = x ? p_blk_two : p_blk, use = x ? p_two : p_run;
                 const bool two = pr.n_rows[1] > 0;
-                // alone, a warp gives back for both
-                auto give = [&](uint64_t* bar) { umma_commit_lead(lead, bar); if (!two && lane == 0) mbar_arrive(bar); };
-                if (x == 0 || two) {
+                if (x == 1 && !two) {
+                    // One tile: the second tile's warp still sees every phase of the barriers and gives back what it has no use for.  (Passing the
+                    // run by, it could reach the next one while this one's copies are in flight, and a wait for the next phase, which has
+                    // the parity of the phase before this one, would pass at once.)
+                    wait(&q_ready_bar[0], (uint32_t)p_run & 1u);
+                    if (lane == 0) mbar_arrive(&q_free_bar[0]);
+                    for (int b = p_blk; b < p_blk + n && ok; ++b) {
+#pragma unroll
+                        for (int ring = 0; ring < 2 * E; ring += E) {
+                            wait(&ready_bar[ring + b % E], (uint32_t)(b / E) & 1u);
+                            if (lane == 0) mbar_arrive(&empty_bar[ring + b % E]);
+                        }
+                    }
+                } else {
                     wait(&q_ready_bar[0], (uint32_t)p_run & 1u);
                     for (int t = -1; t < n && ok; ++t) {
                         // 64 positions at a time: the weights of block t times V, then, over what they left, the scores of block t + 1.  So the
@@ -433,9 +444,9 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             }
                         }
                         if (!ok) break;
-                        if (t >= 0) give(&empty_bar[E + vb % E]);
-                        if (t + 1 < n) give(&empty_bar[kb % E]);
-                        if (t + 2 == n) give(&q_free_bar[0]);
+                        if (t >= 0) umma_commit_lead(lead, &empty_bar[E + vb % E]);
+                        if (t + 1 < n) umma_commit_lead(lead, &empty_bar[kb % E]);
+                        if (t + 2 == n) umma_commit_lead(lead, &q_free_bar[0]);
                     }
                 }
                 p_blk += n;

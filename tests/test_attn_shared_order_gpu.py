@@ -1,0 +1,40 @@
+"""Shared-prefix attention where one CTA goes through many items of different kinds: what a wait stands for must not depend on how far the
+other roles have come.  Against 64 bits, and many calls that have to agree in every bit."""
+import pytest
+import torch
+
+import test_attn_shared as attn
+from test_attn_shared import mv  # noqa: F401  (a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def _same_again(mv, w, times):
+    """The first call's results; the others' have to equal them."""
+    out, out32, lse, status = attn._run(mv, w)
+    assert status == 0
+    for _ in range(times):
+        again = attn._run(mv, w)
+        assert all(torch.equal(x, y) for x, y in zip((out, out32, lse), again)) and again[3] == 0
+    return out, out32, lse
+
+
+# 8 query heads to a KV head and 8 block rows: two sequences to a tile.  5, 6 and 9, 10 and 13, 14 sequences: 3, 5 and 7 tiles, so that an item
+# on one tile ends a group and an item on two begins the next.
+ODD_TILES = [5, 4, 9, 2, 13, 6, 1, 10, 2, 3, 14, 2]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_groups,blocks,hkv", [(256, (1, 2, 3, 4, 5), 1), (256, (1,), 1), (256, (2,), 2), (256, (4, 1), 1), (200, (3, 1, 2), 1), (60, (5, 2, 1, 4, 3), 3), (11, (1, 3, 2), 4)])
+def test_items_on_one_tile_ahead_of_items_on_two(mv, d, n_groups, blocks, hkv):
+    sizes = [ODD_TILES[(i * 5 + 1) % len(ODD_TILES)] for i in range(n_groups)]
+    w = attn._make(sizes, [128 * blocks[i % len(blocks)] for i in range(n_groups)], [0, 3, 20], 7, 8 * hkv, hkv, d, d + n_groups)
+    attn._check(w, *_same_again(mv, w, 30))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sizes", [[11, 21, 32], [2, 21, 1, 11, 32], [3, 30, 3, 12]])
+def test_long_items_on_one_tile(mv, d, sizes):
+    """28 query heads on 4, six rows: three sequences to a tile; long prefixes, so that the ranges of the CTAs cut every kind of item."""
+    w = attn._make(sizes, [2048 + 384 * i for i in range(len(sizes))], [100, 7, 260], 5, 28, 4, d, 3)
+    attn._check(w, *_same_again(mv, w, 10))

@@ -180,6 +180,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __shared__ __align__(8) uint64_t o_full_bar[2], o_free_bar[2];     // by tile
     __shared__ __align__(8) uint64_t pv_done_bar;                      // one tile: O is up to date
     __shared__ __align__(8) uint64_t pv_half_bar[2];                   // by accumulator: it has the first 64 positions of a block
+    __shared__ __align__(8) uint64_t two_done_bar;                     // the second tile's products of all prefix items are done (one phase)
     __shared__ __align__(8) uint64_t run_ready_bar[kRunQueue], run_free_bar[kRunQueue];      // the runs, worked out by the K warp for all
     __shared__ Run s_runs[kRunQueue];
     __shared__ uint32_t tmem_base_slot;
@@ -192,7 +193,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     {
         struct { uint64_t* bar; int n, arrivals; } const kinds[] = {
             {ready_bar, 2 * E, 1}, {empty_bar, 2 * E, NT}, {landed_bar, 2 * E, 1}, {q_ready_bar, 2, 1}, {q_free_bar, 2, NT}, {&s_full_bar[0][0], 4, 1}, {&p_full_bar[0][0], 4, 4},
-            {o_full_bar, 2, 1}, {o_free_bar, 2, 4}, {&pv_done_bar, 1, 1}, {pv_half_bar, 2, 1}, {run_ready_bar, kRunQueue, 1},
+            {o_full_bar, 2, 1}, {o_free_bar, 2, 4}, {&pv_done_bar, 1, 1}, {pv_half_bar, 2, 1}, {&two_done_bar, 1, 1}, {run_ready_bar, kRunQueue, 1},
             {run_free_bar, kRunQueue, 4 + 4 * NT}};                   // V, two helpers, products, softmax
         int at = threadIdx.x;
 #pragma unroll
@@ -452,6 +453,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 p_blk += n;
                 if (two) { p_blk_two += n; ++p_two; }
             }
+            if (x == 1 && p_two > 0) umma_commit_lead(lead, &two_done_bar);
             if (!ok) p_any = false;
         }
     }
@@ -635,7 +637,8 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         Run kr = pr, vr = pr;
         int k_run = p_run, k_t = 0, v_run = p_run, v_t = 0;
         bool any = p_any, have_v = any;
-        if (any && p_two > 0) wait(&o_full_bar[1], (uint32_t)(p_two - 1) & 1u);       // the second tile's products are another warp's
+        // The second tile's products are another warp's.  (That warp may be an item behind: a parity of o_full_bar[1] could be an older phase's.)
+        if (any && p_two > 0) wait(&two_done_bar, 0u);
         int turn = 0, n_s = 0, n_p = 0;                               // tails so far (scores), blocks so far
         while (have_v && ok) {
             if (any && n_s < n_p + 2) {

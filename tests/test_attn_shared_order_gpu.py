@@ -38,3 +38,11 @@ def test_long_items_on_one_tile(mv, d, sizes):
     """28 query heads on 4, six rows: three sequences to a tile; long prefixes, so that the ranges of the CTAs cut every kind of item."""
     w = attn._make(sizes, [2048 + 384 * i for i in range(len(sizes))], [100, 7, 260], 5, 28, 4, d, 3)
     attn._check(w, *_same_again(mv, w, 10))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_groups,size", [(256, 4), (251, 3), (243, 4), (230, 6), (214, 4), (199, 5), (187, 8), (150, 7)])
+def test_tails_behind_short_items_on_two_tiles(mv, d, n_groups, size):
+    """Prefixes of a block or two: one CTA ends several items on two tiles and goes on with tails, which use both tiles' scores and accumulators."""
+    w = attn._make([size] * n_groups, [128 * (1 + i % 2) for i in range(n_groups)], [0, 3, 140], 7, 8, 1, d, n_groups)
+    attn._check(w, *_same_again(mv, w, 30))

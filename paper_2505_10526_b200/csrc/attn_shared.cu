@@ -744,8 +744,10 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                             if (__any_sync(0xffffffffu, factor != 1.f)) {
                                 // O has to be up to date: with the block's first half where this is its second, else with the block before (scores
                                 // in halves: those of this block's second half stand behind it; a tail with two accumulators: this block's do)
+                                // (one tile: the block before comes first in both, since its product may not have begun when this block's scores
+                                // are there, and the parity of pv_half_bar would be that of a phase before)
+                                if (NT == 1 && !mbar_wait_warp(&pv_done_bar, (uint32_t)(tau - 1) & 1u, abort_ptr)) ok = false;
                                 if (h == 1 && !mbar_wait_warp(&pv_half_bar[x], (uint32_t)tau & 1u, abort_ptr)) ok = false;
-                                if (h == 0 && NT == 1 && !mbar_wait_warp(&pv_done_bar, (uint32_t)(tau - 1) & 1u, abort_ptr)) ok = false;
                                 if (h == 0 && halves && !mbar_wait_warp(&s_full_bar[x][1], parity, abort_ptr)) ok = false;
                                 if (!ok) break;
                                 tc_fence_after();

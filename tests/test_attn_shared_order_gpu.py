@@ -46,3 +46,16 @@ def test_tails_behind_short_items_on_two_tiles(mv, d, n_groups, size):
     """Prefixes of a block or two: one CTA ends several items on two tiles and goes on with tails, which use both tiles' scores and accumulators."""
     w = attn._make([size] * n_groups, [128 * (1 + i % 2) for i in range(n_groups)], [0, 3, 140], 7, 8, 1, d, n_groups)
     attn._check(w, *_same_again(mv, w, 30))
+
+
+@pytest.mark.parametrize("d", [256, 128, 64])
+@pytest.mark.parametrize("sizes,shared,tails,gamma,hq,hkv", [([5, 3], [2048, 0], [0, 1900], 3, 16, 8), ([1, 1, 1], [0, 0, 0], [3000, 2500, 200], 5, 16, 8), ([12], [1536], [700, 30], 7, 8, 2), ([40], [0], [500, 900], 1, 16, 8)])
+def test_maxima_that_rise_in_the_second_half_of_every_block(mv, d, sizes, shared, tails, gamma, hq, hkv):
+    """The accumulator is rescaled between a block's halves, each time behind a product that may still be waiting for its V."""
+    w = attn._make(sizes, shared, tails, gamma, hq, hkv, d, 17)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    for b in range(sum(sizes)):
+        for i, page in enumerate(w["page_table"][b].tolist()):
+            if page >= 0 and i % 8 >= 4:                                    # a block is 8 pages; 3 log2 units per block and unit of the row's spread
+                w["k_pages"][page] = (torch.randn((hkv, 16, d), dtype=torch.bfloat16, device="cuda", generator=g).float() * (1 + 3 * (i // 8))).to(torch.bfloat16)
+    attn._check(w, *_same_again(mv, w, 30))

@@ -240,7 +240,7 @@ attn_split_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
     const int L = p.seq_lens[b];
-    if (L < 0 || L + p.R > p.max_pages * kPageSize) {            // no room for the block: skip the sequence
+    if (!has_room(L, p.R, p.max_pages)) {            // no room for the block: skip the sequence
         if (chunk == 0 && g == 0 && threadIdx.x == 0) set_status(p.dev_status, MASSV_ERR_CAPACITY);
         return;
     }
@@ -499,7 +499,7 @@ attn_flat_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     for (int i = threadIdx.x; i < p.B; i += blockDim.x) {
         const int L = p.seq_lens[i];
         int n = 0;
-        if (L < 0 || L + p.R > p.max_pages * kPageSize) {            // no room for the block: skip the sequence
+        if (!has_room(L, p.R, p.max_pages)) {            // no room for the block: skip the sequence
             if (blockIdx.x == 0) set_status(p.dev_status, MASSV_ERR_CAPACITY);
         } else {
             n = (L + p.R + TILE - 1) / TILE - first_tile(L) + kPairUnits;
@@ -747,7 +747,7 @@ __global__ void __launch_bounds__(128) attn_combine_kernel(const AttnParams p, i
     pdl_wait();
     pdl_trigger();
     const int L = p.seq_lens[b];
-    if (L < 0 || L + p.R > p.max_pages * kPageSize) return;
+    if (!has_room(L, p.R, p.max_pages)) return;
     const int first_chunk = (p.window > 0 ? max(0, L - p.window + 1) : 0) / p.kv_chunk;   // as in the split kernel
     const int n_chunks = (L + p.R + p.kv_chunk - 1) / p.kv_chunk - first_chunk;
     if (n_chunks <= 1) return;

@@ -187,7 +187,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     __shared__ int abort_flag;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int R = p.a.R, B = p.a.B, cap = p.a.max_pages * kPageSize;
+    const int R = p.a.R, B = p.a.B;
     const int G = p.a.Hq / p.a.Hkv, nb = kTileRows / G, tile_rows = nb * G;
     // barriers, one thread each (45 initialisations by one thread take 1,100 cycles)
     {
@@ -228,7 +228,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     pdl_wait();
 
     // ---- groups: the least length of the members and their number (gcost, gitem for the moment), the first sequence
-    auto fits = [&](int L) { return L >= 0 && L + R <= cap; };
+    auto fits = [&](int L) { return has_room(L, R, p.a.max_pages); };
     bool bad_here = false;
     {
         // (the first round's loads are all asked for before any is used)

@@ -180,7 +180,7 @@ attn_umma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         for (int i = threadIdx.x; i < p.B; i += blockDim.x) {
             const int L = p.seq_lens[i];
             int n = 0;
-            if (L < 0 || L + p.R > p.max_pages * kPageSize) {       // no room for the block: skip the sequence
+            if (!has_room(L, p.R, p.max_pages)) {       // no room for the block: skip the sequence
                 if (blockIdx.x == 0) set_status(p.dev_status, MASSV_ERR_CAPACITY);
             } else {
                 const int lo_min = p.window > 0 ? max(0, L - p.window + 1) : 0;
@@ -217,7 +217,7 @@ attn_umma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     } else {
         const int b = blockIdx.z, chunk = blockIdx.x;
         const int L = p.seq_lens[b];
-        if (L < 0 || L + p.R > p.max_pages * kPageSize) {
+        if (!has_room(L, p.R, p.max_pages)) {
             if (chunk == 0 && blockIdx.y == 0 && threadIdx.x == 0) set_status(p.dev_status, MASSV_ERR_CAPACITY);
             has_work = false;
         } else {

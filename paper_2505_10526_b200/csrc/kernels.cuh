@@ -31,6 +31,8 @@ struct AttnParams {
     float* flat_part_ml;   // [kFlatMaxCtas * 2, rows_pad, 2]
     int32_t* flat_meta;    // [0] units per CTA (kFlatWholePairs: every pair has a CTA to itself), [1] units of a pair ahead of its tiles, [2 + b] units of sequences 0 .. b-1 (per KV head); a tile is a unit
 };
+// Whether a sequence of L committed positions has room for its block of R rows (lengths come from the device as they are: L + R may overflow).
+__device__ __forceinline__ bool has_room(int L, int R, int max_pages) { return L >= 0 && L <= max_pages * kPageSize - R; }
 constexpr int kFlatMaxCtas = 320;      // resident CTAs of the flat schedule (two per SM)
 constexpr int kFlatMaxBatchMeta = 1024;
 constexpr int kFlatWholePairs = 0x7fffffff;   // more units than any line has: the merge finds every pair in one CTA's range

@@ -59,3 +59,22 @@ def test_maxima_that_rise_in_the_second_half_of_every_block(mv, d, sizes, shared
             if page >= 0 and i % 8 >= 4:                                    # a block is 8 pages; 3 log2 units per block and unit of the row's spread
                 w["k_pages"][page] = (torch.randn((hkv, 16, d), dtype=torch.bfloat16, device="cuda", generator=g).float() * (1 + 3 * (i // 8))).to(torch.bfloat16)
     attn._check(w, *_same_again(mv, w, 30))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("sizes,shared,gamma,hq,hkv", [([3], 512, 0, 2, 1), ([3, 4], 2048, 2, 8, 2), ([40, 30], 256, 3, 16, 8)])
+def test_keys_that_are_no_numbers(mv, d, sizes, shared, gamma, hq, hkv):
+    """A part of a row's context of which no score is a number: the row is none either, and nothing else changes."""
+    w = attn._make(sizes, [shared] * len(sizes), [0], gamma, hq, hkv, d, 21)
+    want = attn._run(mv, w)
+    w["k_new"][1, 0] = float("nan")                                         # all that this sequence's first row has behind the prefix
+    got = attn._run(mv, w)
+    assert got[3] == 0
+    for x, y in zip(got[:3], want[:3]):
+        assert bool(torch.isnan(x[1]).all()) and torch.equal(x[0], y[0]) and torch.equal(x[2:], y[2:])
+    for block in range(shared // 128):                                      # the first group's prefix, a block at a time
+        w = attn._make(sizes, [shared] * len(sizes), [0], gamma, hq, hkv, d, 21)
+        w["k_pages"][w["page_table"][0, block * 8:block * 8 + 8].long()] = float("nan")
+        got = attn._run(mv, w)
+        for x, y in zip(got[:3], want[:3]):
+            assert bool(torch.isnan(x[:sizes[0]]).all()) and torch.equal(x[sizes[0]:], y[sizes[0]:])

@@ -908,8 +908,7 @@ __global__ void __launch_bounds__(SHARE == 1 ? 128 : 256) attn_shared_merge_kern
         for (int i = 0; i < 8; ++i) acc[i] *= keep;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            // (a row may see nothing of a piece, whose sum is then 0; a sum that is no number, of scores that are none, stays one)
-            const float w = ml[i].x == -INFINITY ? ml[i].y * 0.f : exp2f(ml[i].x - m);
+            const float w = ml[i].x == -INFINITY ? 0.f : exp2f(ml[i].x - m);       // (a row may see nothing of a piece)
             sum += ml[i].y * w;
             acc[0] += u[i].x * w; acc[1] += u[i].y * w; acc[2] += u[i].z * w; acc[3] += u[i].w * w;
             acc[4] += v[i].x * w; acc[5] += v[i].y * w; acc[6] += v[i].z * w; acc[7] += v[i].w * w;

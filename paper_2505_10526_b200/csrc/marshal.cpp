@@ -68,6 +68,16 @@ void* here(PyObject* obj, c10::ScalarType dtype) {
     if (obj != Py_None) on_device(obj);
     return pointer(obj, dtype);
 }
+// The same with at least n elements.  (n as a double: no product of a descriptor's fields overflows it; a descriptor whose product is
+// nonsense is the library's to refuse.)
+void* at_least(PyObject* obj, c10::ScalarType dtype, double n, const char* name) {
+    void* data = here(obj, dtype);
+    if ((double)elements(obj) < n && obj != Py_None) {
+        PyErr_Format(PyExc_ValueError, "massv: %s has fewer elements than the call takes", name);
+        throw PythonError();
+    }
+    return data;
+}
 
 // Tokens of heads * d consecutive bf16 elements, evenly spaced: a dense tensor [..., heads, d] or a slice of a fused projection's output.
 struct Tokens { void* data = nullptr; int64_t stride = 0; };
@@ -211,10 +221,12 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const massv_rope_desc& g = *d.get();
         const int64_t count = (int64_t)g.batch * g.rows;
         const uint64_t* turns = static_cast<const uint64_t*>(here(a[1], c10::ScalarType::Long));
+        if (a[1] != Py_None && (int64_t)elements(a[1]) != g.rot_dim / 2) fail(PyExc_ValueError, "massv: turns must have rot_dim / 2 values");
         const Tokens q = tokens_of(a[2], count, g.n_q_heads, g.head_dim), k = tokens_of(a[3], count, g.n_kv_heads, g.head_dim);
         const Tokens qo = tokens_of(a[4], count, g.n_q_heads, g.head_dim), ko = tokens_of(a[5], count, g.n_kv_heads, g.head_dim);
-        int32_t *pos[3];
-        for (int i = 0; i < 3; ++i) pos[i] = static_cast<int32_t*>(here(a[6 + i], c10::ScalarType::Int));
+        const double tokens = (double)g.batch * g.rows;
+        const auto ints = [&](int i, double least, const char* name) { return static_cast<int32_t*>(at_least(a[i], c10::ScalarType::Int, least, name)); };
+        int32_t *const pos[3] = {ints(6, tokens * g.n_axes, "positions"), ints(7, g.batch, "seq_lens"), ints(8, g.batch, "pos_delta")};
         const massv_stream_t s = stream();
         return unlocked([&] { return g_rotary(d.get(), turns, q.data, q.stride, k.data, k.stride, pos[0], pos[1], pos[2], qo.data, qo.stride, ko.data, ko.stride, s); });
     });

@@ -59,6 +59,11 @@ class LogitRules(ctypes.Structure):
                 ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p)]
 
 
+class _SizedRules(LogitRules):
+    """With the lengths of the tensors, in logit_rules' order (-1: None), and their device's index, for the checks of the native marshalling."""
+    _fields_ = [("sizes", ctypes.c_int64 * 10), ("device", ctypes.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python {os.path.join(_PKG, 'build.py')}` "
@@ -156,7 +161,7 @@ def _load_marshal():
     _marshal.bind(address(_lib.massv_verify_attn), address(_lib.massv_accept), address(_lib.massv_kv_commit),
                   address(_lib.massv_sample_top_p), address(_lib.massv_tvd), address(_lib.massv_rotary), address(_lib.massv_verify_attn_shared),
                   address(_lib.massv_logits_apply), address(_lib.massv_accept_logits), address(_lib.massv_history_add),
-                  AttnDesc, AcceptDesc, RopeDesc, LogitRules)
+                  AttnDesc, AcceptDesc, RopeDesc, LogitRules, _SizedRules)
     return _marshal
 
 
@@ -377,15 +382,22 @@ def massv_verify_attn_shared(desc, group_start, shared_lens, q, k_new, v_new, k_
 # ---- rules on logits
 def logit_rules(allowed=None, bias_start=None, bias_tokens=None, bias_values=None, prompt_bits=None, output_bits=None, counts=None, repetition=None,
                 frequency=None, presence=None) -> LogitRules:
-    """Bit masks and indices int32, values fp32 (include/massv.h); the object keeps the tensors alive and is good for any number of calls."""
+    """Bit masks and indices int32, values fp32 (include/massv.h); the object keeps the tensors alive and is good for any number of calls
+    with as many sequences, rows and tokens of vocabulary as they hold, or fewer sequences."""
     f32, i32 = torch.float32, torch.int32
-    r = LogitRules(_ptr(allowed, i32), _ptr(bias_start, i32), _ptr(bias_tokens, i32), _ptr(bias_values, f32), 0, _ptr(prompt_bits, i32), _ptr(output_bits, i32),
+    r = _SizedRules(_ptr(allowed, i32), _ptr(bias_start, i32), _ptr(bias_tokens, i32), _ptr(bias_values, f32), 0, _ptr(prompt_bits, i32), _ptr(output_bits, i32),
                    _ptr(counts, i32), _ptr(repetition, f32), _ptr(frequency, f32), _ptr(presence, f32))
+    tensors = (allowed, bias_start, bias_tokens, bias_values, prompt_bits, output_bits, counts, repetition, frequency, presence)
+    r.sizes[:] = [-1 if t is None else t.numel() for t in tensors]
+    devices = {t.get_device() for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise ValueError("massv: the rules' tensors must live on one device")
+    r.device = devices.pop() if devices else -1
     if bias_tokens is not None:
         if bias_values is None or bias_values.numel() != bias_tokens.numel():
             raise ValueError("massv: bias_tokens and bias_values must have the same length")
         r.n_bias = bias_tokens.numel()
-    r.tensors = (allowed, bias_start, bias_tokens, bias_values, prompt_bits, output_bits, counts, repetition, frequency, presence)
+    r.tensors = tensors
     return r
 
 

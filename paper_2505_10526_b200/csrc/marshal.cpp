@@ -22,7 +22,7 @@ decltype(&massv_verify_attn_shared) g_verify_attn_shared = nullptr;
 decltype(&massv_logits_apply) g_logits_apply = nullptr;
 decltype(&massv_accept_logits) g_accept_logits = nullptr;
 decltype(&massv_history_add) g_history_add = nullptr;
-PyObject *g_attn_desc = nullptr, *g_accept_desc = nullptr, *g_rope_desc = nullptr, *g_logit_rules = nullptr;       // the ctypes structures of the descriptors
+PyObject *g_attn_desc = nullptr, *g_accept_desc = nullptr, *g_rope_desc = nullptr, *g_logit_rules = nullptr, *g_sized_rules = nullptr;       // the ctypes structures of the descriptors
 
 const char* dtype_name(c10::ScalarType t) {
     switch (t) {
@@ -120,6 +120,25 @@ struct DescOf {
     ~DescOf() { PyBuffer_Release(&view); }
     const Desc* get() const { return static_cast<const Desc*>(view.buf); }
 };
+
+// Rules as logit_rules makes them: with the tensors' lengths (-1: no tensor) and their device (-1: no tensors).
+struct SizedRules { massv_logit_rules rules; int64_t sizes[10]; int32_t device; };
+// Whether the rules' tensors are long enough for the call and live where it runs (rules filled in by hand hold bare addresses, as in C).
+void check_rules(PyObject* obj, const massv_logit_rules* rules, int64_t batch, int64_t rows, int64_t vocab) {
+    const int is = PyObject_IsInstance(obj, g_sized_rules);
+    if (is < 0) throw PythonError();
+    if (is == 0 || batch < 1 || rows < 1 || vocab < 1) return;
+    const SizedRules& r = *reinterpret_cast<const SizedRules*>(rules);
+    static const char* const kNames[10] = {"allowed", "bias_start", "bias_tokens", "bias_values", "prompt_bits", "output_bits", "counts", "repetition", "frequency", "presence"};
+    const double words = (double)((vocab + 31) / 32), b = (double)batch;
+    const double need[10] = {b * rows * words, b + 1, 0, 0, b * words, b * words, b * vocab, b, b, b};
+    for (int i = 0; i < 10; ++i)
+        if (r.sizes[i] >= 0 && (double)r.sizes[i] < need[i]) {
+            PyErr_Format(PyExc_ValueError, "massv: the rules' %s has fewer elements than the call's batch and vocabulary take", kNames[i]);
+            throw PythonError();
+        }
+    if (r.device >= 0 && r.device != c10::cuda::current_device()) fail(PyExc_ValueError, "massv: the rules' tensors must live on the current device");
+}
 
 massv_stream_t stream() { return reinterpret_cast<massv_stream_t>(c10::cuda::getCurrentCUDAStream().stream()); }
 
@@ -255,6 +274,7 @@ PyObject* py_logits_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 8, [&] {
         const int32_t batch = (int32_t)integer(a[0]), gamma = (int32_t)integer(a[1]), vocab = (int32_t)integer(a[2]);
         const DescOf<massv_logit_rules> rules(a[3], g_logit_rules);
+        check_rules(a[3], rules.get(), batch, (int64_t)gamma + 1, vocab);
         float *z = static_cast<float*>(here(a[4], c10::ScalarType::Float)), *out = static_cast<float*>(here(a[5], c10::ScalarType::Float));
         int32_t *drafts = static_cast<int32_t*>(here(a[6], c10::ScalarType::Int)), *status = static_cast<int32_t*>(here(a[7], c10::ScalarType::Int));
         const massv_stream_t s = stream();
@@ -265,6 +285,7 @@ PyObject* py_accept_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 13, [&] {
         const DescOf<massv_accept_desc> d(a[0], g_accept_desc);
         const std::unique_ptr<DescOf<massv_logit_rules>> rules(a[1] == Py_None ? nullptr : new DescOf<massv_logit_rules>(a[1], g_logit_rules));
+        if (rules) check_rules(a[1], rules->get(), d.get()->batch, (int64_t)d.get()->gamma + 1, d.get()->vocab);
         const auto f = [&](int i) { return static_cast<float*>(here(a[i], c10::ScalarType::Float)); };
         const auto w = [&](int i) { return static_cast<int32_t*>(here(a[i], c10::ScalarType::Int)); };
         float *z = f(2), *out = f(3);
@@ -291,12 +312,12 @@ PyObject* py_history_add(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* py_bind(PyObject*, PyObject* args) {
     unsigned long long attn, accept, commit, top_p, tvd, rotary, shared, apply, accept_logits, history;
-    PyObject *attn_desc, *accept_desc, *rope_desc, *logit_rules;
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKKO!O!O!O!", &attn, &accept, &commit, &top_p, &tvd, &rotary, &shared, &apply, &accept_logits, &history, &PyType_Type, &attn_desc,
-                          &PyType_Type, &accept_desc, &PyType_Type, &rope_desc, &PyType_Type, &logit_rules))
+    PyObject *attn_desc, *accept_desc, *rope_desc, *logit_rules, *sized_rules;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKO!O!O!O!O!", &attn, &accept, &commit, &top_p, &tvd, &rotary, &shared, &apply, &accept_logits, &history, &PyType_Type, &attn_desc,
+                          &PyType_Type, &accept_desc, &PyType_Type, &rope_desc, &PyType_Type, &logit_rules, &PyType_Type, &sized_rules))
         return nullptr;
     const auto keep = [](PyObject*& slot, PyObject* type) { Py_INCREF(type); Py_XSETREF(slot, type); };
-    keep(g_attn_desc, attn_desc); keep(g_accept_desc, accept_desc); keep(g_rope_desc, rope_desc); keep(g_logit_rules, logit_rules);
+    keep(g_attn_desc, attn_desc); keep(g_accept_desc, accept_desc); keep(g_rope_desc, rope_desc); keep(g_logit_rules, logit_rules); keep(g_sized_rules, sized_rules);
     g_rotary = reinterpret_cast<decltype(g_rotary)>(rotary);
     g_verify_attn_shared = reinterpret_cast<decltype(g_verify_attn_shared)>(shared);
     g_logits_apply = reinterpret_cast<decltype(g_logits_apply)>(apply);

@@ -143,6 +143,11 @@ void check_rules(PyObject* obj, const massv_logit_rules* rules, int64_t batch, i
 massv_stream_t stream() { return reinterpret_cast<massv_stream_t>(c10::cuda::getCurrentCUDAStream().stream()); }
 
 long integer(PyObject* o) { const long v = PyLong_AsLong(o); if (v == -1 && PyErr_Occurred()) throw PythonError(); return v; }
+int32_t int_of(PyObject* o) {                                    // an int32, whole
+    const long v = integer(o);
+    if (v != (int32_t)v) fail(PyExc_OverflowError, "massv: a size does not fit in 32 bits");
+    return (int32_t)v;
+}
 double number(PyObject* o) {                                     // whatever float() takes
     PyObject* f = PyNumber_Float(o);
     if (!f) throw PythonError();
@@ -253,30 +258,35 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* py_verify_attn_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 15, [&] {
         const DescOf<massv_attn_desc> d(a[0], g_attn_desc);
-        const auto in = [&](int i, c10::ScalarType t) { return here(a[i], t); };
+        const massv_attn_desc& g = *d.get();
+        const double rows = (double)g.batch * (g.gamma + 1.0), q_size = rows * g.n_q_heads * g.head_dim, new_size = rows * g.n_kv_heads * g.head_dim;
+        const double pool = (double)g.num_pages * g.n_kv_heads * g.page_size * g.head_dim;
+        const auto in = [&](int i, c10::ScalarType t, double least, const char* name) { return at_least(a[i], t, least, name); };
         constexpr auto BF = c10::ScalarType::BFloat16, I = c10::ScalarType::Int, F = c10::ScalarType::Float;
         if (a[1] == Py_None || a[2] == Py_None) fail(PyExc_ValueError, "massv: groups expected");
-        int32_t *start = static_cast<int32_t*>(in(1, I)), *shared = static_cast<int32_t*>(in(2, I));
+        int32_t *start = static_cast<int32_t*>(here(a[1], I)), *shared = static_cast<int32_t*>(here(a[2], I));
         const int64_t groups = THPVariable_Unpack(a[2]).numel();
         if (THPVariable_Unpack(a[1]).numel() != groups + 1) fail(PyExc_ValueError, "massv: group_start has one entry more than shared_lens");
-        void *q = in(3, BF), *kn = in(4, BF), *vn = in(5, BF), *kp = in(6, BF), *vp = in(7, BF);
-        int32_t *table = static_cast<int32_t*>(in(8, I)), *lens = static_cast<int32_t*>(in(9, I));
-        void* out = in(10, BF);
-        float *out32 = static_cast<float*>(in(11, F)), *lse = static_cast<float*>(in(12, F));
-        void* ws = in(13, c10::ScalarType::Undefined);
+        void *q = in(3, BF, q_size, "q"), *kn = in(4, BF, new_size, "k_new"), *vn = in(5, BF, new_size, "v_new"), *kp = in(6, BF, pool, "k_pages"), *vp = in(7, BF, pool, "v_pages");
+        int32_t *table = static_cast<int32_t*>(in(8, I, (double)g.batch * g.max_pages_per_seq, "page_table")), *lens = static_cast<int32_t*>(in(9, I, g.batch, "seq_lens"));
+        void* out = in(10, BF, q_size, "out");
+        float *out32 = static_cast<float*>(in(11, F, q_size, "out_f32")), *lse = static_cast<float*>(in(12, F, rows * g.n_q_heads, "lse"));
+        void* ws = here(a[13], c10::ScalarType::Undefined);
         const size_t ws_bytes = elements(a[13]);
-        int32_t* status = static_cast<int32_t*>(in(14, I));
+        int32_t* status = static_cast<int32_t*>(in(14, I, 1, "dev_status"));
         const massv_stream_t s = stream();
         return unlocked([&] { return g_verify_attn_shared(d.get(), (int32_t)groups, start, shared, q, kn, vn, kp, vp, table, lens, out, out32, lse, ws, ws_bytes, status, s); });
     });
 }
 PyObject* py_logits_apply(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 8, [&] {
-        const int32_t batch = (int32_t)integer(a[0]), gamma = (int32_t)integer(a[1]), vocab = (int32_t)integer(a[2]);
+        const int32_t batch = int_of(a[0]), gamma = int_of(a[1]), vocab = int_of(a[2]);
         const DescOf<massv_logit_rules> rules(a[3], g_logit_rules);
         check_rules(a[3], rules.get(), batch, (int64_t)gamma + 1, vocab);
-        float *z = static_cast<float*>(here(a[4], c10::ScalarType::Float)), *out = static_cast<float*>(here(a[5], c10::ScalarType::Float));
-        int32_t *drafts = static_cast<int32_t*>(here(a[6], c10::ScalarType::Int)), *status = static_cast<int32_t*>(here(a[7], c10::ScalarType::Int));
+        constexpr auto I = c10::ScalarType::Int, F = c10::ScalarType::Float;
+        const double size = (double)batch * (gamma + 1.0) * vocab;
+        float *z = static_cast<float*>(at_least(a[4], F, size, "logits")), *out = static_cast<float*>(at_least(a[5], F, size, "logits_out"));
+        int32_t *drafts = static_cast<int32_t*>(at_least(a[6], I, (double)batch * gamma, "draft_tokens")), *status = static_cast<int32_t*>(at_least(a[7], I, 1, "dev_status"));
         const massv_stream_t s = stream();
         return unlocked([&] { return g_logits_apply(batch, gamma, vocab, rules.get(), z, out, drafts, status, s); });
     });
@@ -286,25 +296,28 @@ PyObject* py_accept_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const DescOf<massv_accept_desc> d(a[0], g_accept_desc);
         const std::unique_ptr<DescOf<massv_logit_rules>> rules(a[1] == Py_None ? nullptr : new DescOf<massv_logit_rules>(a[1], g_logit_rules));
         if (rules) check_rules(a[1], rules->get(), d.get()->batch, (int64_t)d.get()->gamma + 1, d.get()->vocab);
-        const auto f = [&](int i) { return static_cast<float*>(here(a[i], c10::ScalarType::Float)); };
-        const auto w = [&](int i) { return static_cast<int32_t*>(here(a[i], c10::ScalarType::Int)); };
-        float *z = f(2), *out = f(3);
-        int32_t* drafts = w(4);
-        float *q = f(5), *ua = f(6), *us = f(7);
-        int32_t *tokens = w(8), *lens = w(9);
-        float* probs = f(10);
+        const double batch = d.get()->batch, drafted = batch * d.get()->gamma, rows = drafted + batch, vocab = d.get()->vocab;
+        const auto f = [&](int i, double least, const char* name) { return static_cast<float*>(at_least(a[i], c10::ScalarType::Float, least, name)); };
+        const auto w = [&](int i, double least, const char* name) { return static_cast<int32_t*>(at_least(a[i], c10::ScalarType::Int, least, name)); };
+        float *z = f(2, rows * vocab, "logits"), *out = f(3, rules ? rows * vocab : 0, "logits_out");
+        int32_t* drafts = w(4, drafted, "draft_tokens");
+        const double sampling = d.get()->temperature > 0.f ? 1 : 0;          // (not read at T = 0)
+        float *q = f(5, sampling * drafted * vocab, "draft_probs"), *ua = f(6, sampling * drafted, "u_accept"), *us = f(7, sampling * rows, "u_sample");
+        int32_t *tokens = w(8, rows, "out_tokens"), *lens = w(9, batch, "accept_len");
+        float* probs = f(10, rows * vocab, "probs_out");
         void* ws = here(a[11], c10::ScalarType::Undefined);
         const size_t ws_bytes = elements(a[11]);
-        int32_t* status = w(12);
+        int32_t* status = w(12, 1, "dev_status");
         const massv_stream_t s = stream();
         return unlocked([&] { return g_accept_logits(d.get(), rules ? rules->get() : nullptr, z, out, drafts, q, ua, us, tokens, lens, probs, ws, ws_bytes, status, s); });
     });
 }
 PyObject* py_history_add(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 8, [&] {
-        const int32_t batch = (int32_t)integer(a[0]), vocab = (int32_t)integer(a[1]), n_max = (int32_t)integer(a[3]);
-        const auto w = [&](int i) { return static_cast<int32_t*>(here(a[i], c10::ScalarType::Int)); };
-        int32_t *tokens = w(2), *lens = w(4), *bits = w(5), *counts = w(6), *status = w(7);
+        const int32_t batch = int_of(a[0]), vocab = int_of(a[1]), n_max = int_of(a[3]);
+        const auto w = [&](int i, double least, const char* name) { return static_cast<int32_t*>(at_least(a[i], c10::ScalarType::Int, least, name)); };
+        int32_t *tokens = w(2, (double)batch * n_max, "tokens"), *lens = w(4, batch, "lens"), *bits = w(5, (double)batch * ((vocab + 31LL) / 32), "bits"),
+                *counts = w(6, (double)batch * vocab, "counts"), *status = w(7, 1, "dev_status");
         const massv_stream_t s = stream();
         return unlocked([&] { return g_history_add(batch, vocab, tokens, n_max, lens, reinterpret_cast<uint32_t*>(bits), counts, status, s); });
     });

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import test_attn_shared as attn
 import test_logit_rules as rules_of
 from test_rotary import mv  # noqa: F401  (a fixture)
 
@@ -90,3 +91,52 @@ def test_rules_of_another_batch_or_vocabulary(mv):
     rules.device += 1                                                       # as tensors of another device would note
     with pytest.raises(ValueError, match="current device"):
         apply(s["logits"], rules)
+
+
+# ---------------------------------------------------------------- the other tensors
+@pytest.mark.gpu
+def test_shared_attention_tensors(mv):
+    w = attn._make([3, 2], [256, 130], [10, 4], 2, 8, 2, 64, 1)
+    batch, rows, hq, d = w["q"].shape
+    desc = mv.attn_desc(batch, rows - 1, hq, 2, d, w["page_table"].shape[1], w["k_pages"].shape[0])
+    ws = mv.alloc_workspace(mv.massv_verify_attn_shared_workspace_size(desc, 2), "cuda")
+    names = ("q", "k_new", "v_new", "k_pages", "v_pages", "page_table", "seq_lens", "out", "out_f32", "lse", "dev_status")
+    good = {n: w[n] for n in names[:7]}
+    good.update(out=torch.empty_like(w["q"]), out_f32=torch.empty(w["q"].shape, device="cuda"), lse=torch.empty((batch, rows, hq), device="cuda"), dev_status=_ints(1))
+    _refused(lambda **kw: mv.massv_verify_attn_shared(desc, w["start"], w["shared"], workspace=ws, **kw), good, names, {n: f"{n} has fewer elements" for n in names})
+    assert int(good["dev_status"].item()) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [0.0, 1.0])
+def test_acceptance_tensors(mv, T):
+    batch, gamma, vocab = 3, 2, 2048
+    s = rules_of._make(batch, gamma, vocab, ("history",), 5)
+    desc, rules = mv.accept_desc(batch, gamma, 64, vocab, T), rules_of._rules(mv, s)
+    ws = mv.alloc_workspace(mv.massv_accept_logits_workspace_size(desc), "cuda")
+    good = dict(logits=s["logits"], logits_out=torch.empty_like(s["logits"]), draft_tokens=s["draft_tokens"], draft_probs=torch.softmax(s["logits"][:, :gamma], -1).contiguous(),
+                u_accept=torch.rand((batch, gamma), device="cuda"), u_sample=torch.rand((batch, gamma + 1), device="cuda"), out_tokens=_ints(batch, gamma + 1), accept_len=_ints(batch),
+                probs_out=torch.empty_like(s["logits"]), dev_status=_ints(1))
+    names = list(good)
+    if T == 0:
+        good["probs_out"] = None
+        names = [n for n in names if n not in ("probs_out", "draft_probs", "u_accept", "u_sample")]          # (not read)
+        for n in ("draft_probs", "u_accept", "u_sample"):
+            good[n] = good[n].flatten()[:1].clone()
+    _refused(lambda **kw: mv.massv_accept_logits(desc, rules, workspace=ws, **kw), good, names, {n: f"{n} has fewer elements" for n in names})
+    mv.massv_accept_logits(desc, None, workspace=ws, **dict(good, logits_out=good["logits_out"].flatten()[:4]))       # without rules nothing is written there
+    assert int(good["dev_status"].item()) == 0
+
+
+@pytest.mark.gpu
+def test_apply_and_history_tensors(mv):
+    batch, gamma, vocab, n = 3, 2, 1001, 4
+    s = rules_of._make(batch, gamma, vocab, ("history",), 5)
+    out = torch.empty_like(s["logits"])
+    apply = lambda **kw: mv.massv_logits_apply(gamma, rules_of._rules(mv, s), s["logits"], out, **kw)
+    _refused(apply, dict(draft_tokens=s["draft_tokens"], dev_status=_ints(1)), ("draft_tokens", "dev_status"), dict(draft_tokens="draft_tokens has fewer", dev_status="dev_status has fewer"))
+    add = lambda **kw: mv.massv_history_add(vocab, _ints(batch, n), **kw)
+    good = dict(lens=_ints(batch), bits=_ints(batch, 32), counts=_ints(batch, vocab), dev_status=_ints(1))
+    _refused(add, good, list(good), {name: f"{name} has fewer elements" for name in good})
+    with pytest.raises(OverflowError):
+        mv.massv_history_add(2 ** 32 + vocab, _ints(batch, n), None, good["bits"])

@@ -397,7 +397,7 @@ def logit_rules(allowed=None, bias_start=None, bias_tokens=None, bias_values=Non
         if bias_values is None or bias_values.numel() != bias_tokens.numel():
             raise ValueError("massv: bias_tokens and bias_values must have the same length")
         r.n_bias = bias_tokens.numel()
-    r.tensors = tensors
+    r.tensors, r.history = tensors, (output_bits, counts)
     return r
 
 

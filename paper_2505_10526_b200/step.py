@@ -29,8 +29,8 @@ class VerifyStep:
         """``rope``: None, or the keyword arguments of ``rope_desc`` from ``rot_dim`` on together with ``turns``
         (massv_rope_frequencies); the step's inputs may then hold ``pos_delta`` (int32 [B]).
         ``n_groups`` > 0: the inputs hold ``group_start`` and ``shared_lens``.
-        ``rules``: the inputs hold ``rules`` (``logit_rules``), and ``run`` adds the emitted tokens to ``output_bits`` and
-        ``counts`` where the inputs hold them."""
+        ``rules``: the inputs hold ``rules`` (``logit_rules``), and ``run`` adds the emitted tokens to the history that they read, or to
+        ``output_bits`` and ``counts`` of the inputs where these are given."""
         self.device = torch.device(device)
         self.B, self.gamma, self.R = batch, gamma, gamma + 1
         self.T = float(temperature)
@@ -108,8 +108,15 @@ class VerifyStep:
         mv.massv_kv_commit(self.B, self.gamma, None if rollback else self.accept_len, seq_lens, self.dev_status)
 
     def record(self, w):
-        """The step's emitted tokens into the history that the rules read."""
-        mv.massv_history_add(self.vocab, self.out_tokens, self.accept_len, w["output_bits"], w.get("counts"), self.dev_status)
+        """The step's emitted tokens into the history that the rules read; nothing to do where they read none."""
+        bits, counts = w.get("output_bits"), w.get("counts")
+        own_bits, own_counts = getattr(w["rules"], "history", (None, None))
+        if bits is None:
+            bits, counts = own_bits, own_counts if counts is None else counts
+        elif counts is None and own_bits is not None and bits.data_ptr() == own_bits.data_ptr():
+            counts = own_counts
+        if bits is not None:
+            mv.massv_history_add(self.vocab, self.out_tokens, self.accept_len, bits, counts, self.dev_status)
 
     def run(self, w, commit=True):
         """Enqueue one whole step on the current stream (no synchronisation)."""
@@ -119,7 +126,7 @@ class VerifyStep:
         self.accept(w)
         if commit:
             self.commit(w["seq_lens"])
-            if self.rules and w.get("output_bits") is not None:
+            if self.rules:
                 self.record(w)
 
     # -- end-to-end step with host buffers ----------------------------------------------

@@ -271,15 +271,16 @@ int massv_tvd(const massv_accept_desc *desc, const float *logits, const float *d
               void *workspace, size_t workspace_bytes, int32_t *dev_status, massv_stream_t stream);
 
 /*
- * The same diagnostic (Eq. 6) right after massv_accept on the same stream, with ONE read of the logits:
- * massv_accept leaves every row's merged softmax statistics (max logit, sum of exp((z - max)/T)) in its
+ * The same diagnostic (Eq. 6) right after massv_accept or massv_accept_logits on the same stream, with ONE read of the logits:
+ * the acceptance leaves every row's merged softmax statistics (max logit, sum of exp((z - max)/T)) in its
  * workspace, and this call takes them from there instead of computing them again, so it reads each
  * drafted row of the logits and of q once (B*gamma*V*8 bytes).
- *   desc                  the descriptor massv_accept was called with (T > 0, gamma >= 1)
- *   logits                the logits_out of that massv_accept call
- *   accept_workspace      the workspace of that call, untouched since (its size is checked)
+ *   desc                  the descriptor of the acceptance call (T > 0, gamma >= 1)
+ *   logits                the logits_out of that call (massv_accept_logits without rules: its logits); under rules the distance
+ *                         is that of the distribution the rules leave
+ *   accept_workspace      the workspace of that call, untouched since (at least B * R * 8 bytes, rounded up to 256, are needed)
  *   tvd_out, accept_prob_out, workspace (massv_tvd_workspace_size bytes): as for massv_tvd
- * The statistics come from the LM-head kernel's fp32 arithmetic; results agree with massv_tvd's to
+ * The statistics come from the fp32 arithmetic of the acceptance's first pass; results agree with massv_tvd's to
  * rounding (both are held to 1e-4 absolute against a double-precision evaluation).
  */
 int massv_tvd_after_accept(const massv_accept_desc *desc, const float *logits, const float *draft_probs,

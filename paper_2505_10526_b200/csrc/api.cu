@@ -170,9 +170,13 @@ int check_accept_desc(const massv_accept_desc* d) {
     return MASSV_OK;
 }
 
+// The rows' softmax statistics (maximum and sum of each row) come first in the workspace of either acceptance call: massv_tvd_after_accept
+// takes them from there, whichever it was.
+size_t rowstat_bytes(const massv_accept_desc& d) { return align_up((size_t)d.batch * (d.gamma + 1) * 2 * sizeof(float), kAlign); }
+
 struct AcceptLayout {
     int n_part, n_chunks;
-    size_t off_max, off_sum, off_idx, off_state, off_chunks, off_segs, off_counters, off_rowstat, off_logits, total;
+    size_t off_max, off_sum, off_idx, off_state, off_chunks, off_segs, off_counters, off_logits, total;
 };
 
 AcceptLayout accept_layout(const massv_accept_desc& d) {
@@ -180,7 +184,7 @@ AcceptLayout accept_layout(const massv_accept_desc& d) {
     const size_t M = (size_t)d.batch * (d.gamma + 1);
     l.n_part = lm_head_num_partials((int)M, d.vocab);
     l.n_chunks = (d.vocab + kResidualChunk - 1) / kResidualChunk;
-    size_t off = 0;
+    size_t off = rowstat_bytes(d);
     l.off_max = off; off += align_up((size_t)l.n_part * M * sizeof(float), kAlign);
     l.off_sum = off; off += align_up((size_t)l.n_part * M * sizeof(float), kAlign);
     l.off_idx = off; off += align_up((size_t)l.n_part * M * sizeof(int32_t), kAlign);
@@ -189,7 +193,6 @@ AcceptLayout accept_layout(const massv_accept_desc& d) {
     l.off_segs = off;
     if (d.temperature > 0.f) off += align_up((size_t)d.batch * l.n_chunks * kResidualSegments * sizeof(double), kAlign);
     l.off_counters = off; off += align_up((size_t)d.batch * sizeof(unsigned int), kAlign);
-    l.off_rowstat = off; off += align_up(M * 2 * sizeof(float), kAlign);
     l.off_logits = off;
     if (d.temperature > 0.f) off += align_up(M * (size_t)d.vocab * sizeof(float), kAlign);
     l.total = off;
@@ -306,7 +309,7 @@ int massv_accept(const massv_accept_desc* desc, const void* hidden, const void* 
     a.chunk_sums = reinterpret_cast<double*>(ws + l.off_chunks);
     a.seg_sums = desc->temperature > 0.f ? reinterpret_cast<double*>(ws + l.off_segs) : nullptr;
     a.counters = reinterpret_cast<unsigned int*>(ws + l.off_counters);
-    a.row_stats = reinterpret_cast<float*>(ws + l.off_rowstat);
+    a.row_stats = reinterpret_cast<float*>(ws);
     a.n_chunks = l.n_chunks;
     a.dev_status = dev_status;
     return launch_accept(a, s) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;
@@ -525,10 +528,9 @@ int massv_tvd_after_accept(const massv_accept_desc* desc, const float* logits, c
                            void* workspace, size_t workspace_bytes, int32_t* dev_status, massv_stream_t stream) {
     const int rc = check_accept_desc(desc);
     if (rc != MASSV_OK) return rc;
-    const AcceptLayout l = accept_layout(*desc);
-    if (!accept_workspace || (reinterpret_cast<uintptr_t>(accept_workspace) % kAlign) != 0 || accept_workspace_bytes < l.total)
+    if (!accept_workspace || (reinterpret_cast<uintptr_t>(accept_workspace) % kAlign) != 0 || accept_workspace_bytes < rowstat_bytes(*desc))
         return MASSV_ERR_WORKSPACE;
-    const float* row_stats = reinterpret_cast<const float*>(static_cast<const char*>(accept_workspace) + l.off_rowstat);
+    const float* row_stats = static_cast<const float*>(accept_workspace);
     return tvd_call(desc, logits, draft_probs, row_stats, tvd_out, accept_prob_out, workspace, workspace_bytes, dev_status, stream);
 }
 
@@ -652,14 +654,14 @@ void set_rules(LogitsParams& p, const massv_logit_rules* r, const int32_t* draft
 
 struct AcceptLogitsLayout {
     int n_part, n_chunks;
-    size_t off_max, off_sum, off_idx, off_state, off_chunks, off_segs, off_counters, off_rowstat, total;
+    size_t off_max, off_sum, off_idx, off_state, off_chunks, off_segs, off_counters, total;
 };
 AcceptLogitsLayout accept_logits_layout(const massv_accept_desc& d) {
     AcceptLogitsLayout l;
     const size_t M = (size_t)d.batch * (d.gamma + 1);
     l.n_part = logit_slices(d.vocab);
     l.n_chunks = (d.vocab + kResidualChunk - 1) / kResidualChunk;
-    size_t off = 0;
+    size_t off = rowstat_bytes(d);
     auto take = [&](size_t bytes) { const size_t at = off; off += align_up(bytes, kAlign); return at; };
     l.off_max = take((size_t)l.n_part * M * sizeof(float));
     l.off_sum = take((size_t)l.n_part * M * sizeof(float));
@@ -668,7 +670,6 @@ AcceptLogitsLayout accept_logits_layout(const massv_accept_desc& d) {
     l.off_chunks = take((size_t)d.batch * l.n_chunks * sizeof(double));
     l.off_segs = take(d.temperature > 0.f ? (size_t)d.batch * l.n_chunks * kResidualSegments * sizeof(double) : 0);
     l.off_counters = take((size_t)d.batch * sizeof(unsigned int));
-    l.off_rowstat = take(M * 2 * sizeof(float));
     l.total = off;
     return l;
 }
@@ -747,7 +748,7 @@ int massv_accept_logits(const massv_accept_desc* desc, const massv_logit_rules* 
     a.chunk_sums = reinterpret_cast<double*>(ws + l.off_chunks);
     a.seg_sums = sampling ? reinterpret_cast<double*>(ws + l.off_segs) : nullptr;
     a.counters = reinterpret_cast<unsigned int*>(ws + l.off_counters);
-    a.row_stats = reinterpret_cast<float*>(ws + l.off_rowstat);
+    a.row_stats = reinterpret_cast<float*>(ws);
     a.n_chunks = l.n_chunks;
     a.dev_status = dev_status;
     return launch_accept(a, s) == cudaSuccess ? MASSV_OK : MASSV_ERR_CUDA;

@@ -462,7 +462,7 @@ int massv_accept_logits(const massv_accept_desc *desc, const massv_logit_rules *
  * lens[b] count (lens NULL: all n_max).  With out_tokens, gamma + 1 and accept_len of an acceptance call it takes a step's
  * result into output_bits and counts; with prompts and counts NULL it fills prompt_bits.  Tokens outside [0, V) and lengths outside
  * [0, n_max] (taken as the nearest bound) store MASSV_ERR_INVALID_ARG.  bits uint32 [B, W], counts int32 [B, V], zeroed by the
- * caller at a request's start.  n_max >= 0; no workspace.
+ * caller at a request's start.  n_max >= 0, batch * n_max <= 2^38; no workspace.
  */
 int massv_history_add(int32_t batch, int32_t vocab, const int32_t *tokens, int32_t n_max, const int32_t *lens,
                       uint32_t *bits, int32_t *counts, int32_t *dev_status, massv_stream_t stream);

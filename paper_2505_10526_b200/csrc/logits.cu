@@ -219,12 +219,13 @@ __global__ void __launch_bounds__(256) history_add_kernel(int B, int V, const in
     const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     pdl_wait();
     pdl_trigger();
-    if (i >= (long long)B * n_max) return;
-    const int b = (int)(i / n_max), k = (int)(i % n_max);
+    const int per = max(n_max, 1);                                // (without tokens: a thread a sequence, for its length)
+    if (i >= (long long)B * per) return;
+    const int b = (int)(i / per), k = (int)(i % per);
     if (lens) {
         const int n = lens[b];
         if (k == 0 && (n < 0 || n > n_max)) set_status(dev_status, MASSV_ERR_INVALID_ARG);
-        if (k >= n) return;
+        if (k >= min(n, n_max)) return;
     }
     const int t = tokens[i];
     if (t < 0 || t >= V) { set_status(dev_status, MASSV_ERR_INVALID_ARG); return; }
@@ -258,8 +259,8 @@ cudaError_t launch_logit_rules(const LogitsParams& p, cudaStream_t stream) {
 
 cudaError_t launch_history_add(int B, int V, const int32_t* tokens, int n_max, const int32_t* lens, uint32_t* bits, int32_t* counts,
                                int32_t* dev_status, cudaStream_t stream) {
-    const long long n = (long long)B * n_max;
-    if (n == 0) return cudaSuccess;
+    if (n_max == 0 && !lens) return cudaSuccess;                  // nothing to add and nothing to report
+    const long long n = (long long)B * (n_max > 0 ? n_max : 1);
     const cudaError_t e = launch_pdl(history_add_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, B, V, tokens, n_max, lens, bits, counts, dev_status);
     if (e != cudaSuccess) return e;
     count_launches(1);

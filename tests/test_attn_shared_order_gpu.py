@@ -78,3 +78,16 @@ def test_keys_that_are_no_numbers(mv, d, sizes, shared, gamma, hq, hkv):
         got = attn._run(mv, w)
         for x, y in zip(got[:3], want[:3]):
             assert bool(torch.isnan(x[:sizes[0]]).all()) and torch.equal(x[sizes[0]:], y[sizes[0]:])
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("factor", [0.25, 4.0])
+def test_an_explicit_scale(mv, d, factor):
+    """A power of two times 1 / sqrt(d) is the same as queries times that power."""
+    w = attn._make([4, 3], [512, 200], [9, 40], 3, 8, 2, d, 8)
+    desc = mv.attn_desc(7, 3, 8, 2, d, w["page_table"].shape[1], w["k_pages"].shape[0], scale=factor * d ** -0.5)
+    ws = mv.alloc_workspace(mv.massv_verify_attn_shared_workspace_size(desc, 2), "cuda").fill_(0xff)
+    out, out32, lse, status = torch.empty_like(w["q"]), torch.empty(w["q"].shape, device="cuda"), torch.empty(w["q"].shape[:3], device="cuda"), torch.zeros((1,), dtype=torch.int32, device="cuda")
+    mv.massv_verify_attn_shared(desc, w["start"], w["shared"], w["q"], w["k_new"], w["v_new"], w["k_pages"], w["v_pages"], w["page_table"], w["seq_lens"], out, out32, lse, ws, status)
+    assert int(status.item()) == 0
+    attn._check(dict(w, q=w["q"] * factor), out, out32, lse)

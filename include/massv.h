@@ -153,6 +153,15 @@ size_t massv_verify_attn_shared_workspace_size(const massv_attn_desc *desc, int3
  *                   its window, with massv_verify_attn on the same page tables); desc->kv_chunk and the kernel choice are not used
  * A group of one sequence, and what a group shares beyond whole blocks of 128 positions, are read per sequence.  A
  * sequence whose lengths violate the capacity rule is skipped, as in massv_verify_attn, and does not count as a member.
+ * Size: with G = n_q_heads / n_kv_heads, (B R / floor(128 / G) + n_groups + B) * n_kv_heads * (max_pages_per_seq / 8 + 1) is at most
+ * 2 * 10^8 (MASSV_ERR_UNSUPPORTED beyond, workspace size 0): the kernel counts the cost of all blocks in 32 bits.
+ * Math: scores, maxima, sums and accumulators in fp32; the softmax's weights are rounded to bf16 for the product with V (2^-8 of
+ * each at most), relative to a running maximum that may lag by a factor of 2^8.  massv_verify_attn rounds them the same way, on short
+ * contexts relative to each tile's own maximum, so the two agree to that rounding, not in every bit.
+ * When to call it (head_dim 64, 128 and 256, 2 to 64 sequences, prefixes of 128 to 16,384 positions, tails of 0 to 3,000): it was the
+ * faster of the two where sharing saves 120 MB or more of K and V reads and these are a third or more of what
+ * massv_verify_attn reads, by up to 4.8 times.  Below 50 MB it was mostly the slower one: groups of one, short prefixes and tails much longer than
+ * the prefix take 1.0 to 1.3 times as long, calls that take massv_verify_attn less than 30 us up to 10 us longer.
  */
 int massv_verify_attn_shared(const massv_attn_desc *desc, int32_t n_groups, const int32_t *group_start, const int32_t *shared_lens,
                              const void *q, const void *k_new, const void *v_new,
@@ -381,8 +390,8 @@ typedef struct massv_rope_scaling {
 
 /*
  * Host only: the frequencies in the form massv_rotary takes, turns per position as a 64-bit fraction (f_i / (2 pi) mod 1, times
- * 2^64), into the HOST array turns[rot_dim / 2].  The product with a position then wraps where the angle does, so that an angle is
- * as exact at position 10^9 as at 1.  scaling NULL: none.  base > 1 (not read with GIVEN).
+ * 2^64), into the HOST array turns[rot_dim / 2].  The product with a position then wraps where the angle does, and an angle is off by no
+ * more than 16 * 2^-64 of a turn per position (at 10^9: 2^-30 of a turn).  scaling NULL: none.  base > 1 (not read with GIVEN).
  */
 int massv_rope_frequencies(int32_t rot_dim, double base, const massv_rope_scaling *scaling, uint64_t *turns);
 
@@ -396,7 +405,8 @@ int massv_rope_frequencies(int32_t rot_dim, double base, const massv_rope_scalin
  *                  of 8, at least n_q_heads * d): a slice of a fused projection's output is taken as it is, and packed on the way out.
  *                  q_out may be q (same stride); otherwise the two do not overlap.  k, k_out alike.
  *   positions      int32 [B * rows, n_axes] or NULL;  seq_lens int32 [B] or NULL (one of the two);  pos_delta int32 [B] or NULL
- * Math: angles exact to 2^-62 of a turn, sine and cosine and products in fp32, one rounding to bf16.  No workspace.
+ * Math: the angle is off by what `turns` is off times the position (massv_rope_frequencies; the product itself is exact modulo a turn) and by
+ * 2^-26 of a turn from its rounding to fp32; sine and cosine and products in fp32, one rounding to bf16.  No workspace.
  */
 int massv_rotary(const massv_rope_desc *desc, const uint64_t *turns, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                  const int32_t *positions, const int32_t *seq_lens, const int32_t *pos_delta,

@@ -28,10 +28,13 @@
 // SM: prefix items, which the tensor cores bound, and tails, which memory bounds, are at work at the same time.  What a CTA has
 // of an item is a piece (O, m, l); attn_shared_merge_kernel adds the pieces of every row up, in order.
 //
-// What bounds it: a two-tile block is 2,048 cycles of products (64 for each 128 x 128 x 16; 48 instead of 32 for one of 64 scores,
-// whose operands shared memory cannot deliver faster) and 2,048 of exponentials, and takes about 3,300: products,
-// copies and tensor-memory traffic share one shared memory.  A prefix alone (64 sequences of 6 rows, 28 heads of 128, 16,384
-// positions) runs at 770 TFLOP/s, tails alone (64 of 1,000 positions, 16 heads of 256) at 5.3 TB/s of K and V.
+// What bounds it: a two-tile block at head_dim 128 is 2,560 cycles of products (64 for each 128 x 128 x 16 with V; 48 instead of 32 for one of 64
+// scores, whose operands shared memory cannot deliver faster) and 2,048 of exponentials, and takes about 3,300: products,
+// copies and tensor-memory traffic share one shared memory.  At 64 the products are 1,280 cycles and the exponentials, as many as before, are
+// the floor (1.1 PFLOP/s).  At 256 one tile's products (2,048) and softmax take turns.  Kernel alone, 64 sequences of 6 rows: prefixes (28 / 4
+// heads of 64 and of 128 behind 16,384 positions, 16 / 8 of 256 behind 8,192) at 430, 770 and 445 TFLOP/s; tails (28 / 4 of 64 and of 128,
+// 2,000 positions each, 16 / 8 of 256, 1,000) at 2.4, 3.7 and 5.3 TB/s of K and V: a block's chain of scores, softmax and product is
+// exposed with two blocks in flight, the more the fewer bytes a block has.
 #include "kernels.cuh"
 #include "ptx.cuh"
 #include "umma.cuh"
@@ -45,8 +48,9 @@ constexpr int kPagesPerBlock = kPrefixBlock / kPageSize;
 constexpr float kRescaleThreshold = 8.f;   // log2 units a row's maximum may outgrow its reference by
 
 // Cost of a block: products of two tiles, of one, of a tail; and what an item costs beside its blocks (queries, write-out).  Set by
-// measurement: equal ranges should take equal time (64 sequences of 28 heads of 128 in three groups, prefixes up
-// to 16,384: 129 us, with 7 for two tiles and 8 for a tail 137; 31 of 16 heads of 256, two groups up to 4,111: 62 us, with 7 for one tile 64).
+// measurement: equal ranges should take equal time (calls back to back on the same inputs: 64 sequences of 28 heads of 128 in three groups, prefixes
+// up to 16,384: 129 us, with 7 for two tiles and 8 for a tail 137; 31 of 16 heads of 256, two groups up to 4,111: 62 us, with 7 for one tile 64).
+// One set serves all head dimensions; it was not fitted to 64, nor to calls of mostly tails.
 constexpr int kCostTwo = 8, kCostOne = 6, kCostTail = 7, kCostPrefixItem = 8, kCostTailItem = 5;
 constexpr int kCostMost = kCostTwo + kCostPrefixItem;
 

@@ -68,7 +68,7 @@ struct SharedAttnParams {
     float *part_o, *part_ml;           // [slots.rows(), d], [slots.rows(), 2]: pieces
     // for the merge
     int32_t* meta;                     // [0] cost of a range, [1] cost of all prefix items
-    int4* seqs;                        // [B] tail blocks of earlier sequences (per KV head), own, first pair within the group, blocks of its prefix
+    int4* seqs;                        // [B] cost of the tails of earlier sequences (per KV head), own tail blocks, first pair within the group, blocks of its prefix
     int4* seq_groups;                  // [B] cost of earlier groups, their items, cost of a block of the group
 };
 SharedAttnSlots shared_attn_slots(int B, int R, int Hq, int Hkv, int d, int n_groups);

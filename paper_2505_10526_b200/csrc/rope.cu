@@ -1,9 +1,9 @@
 // Rotary positions of queries and keys (massv_rotary).
 //
 // A CTA takes a few tokens.  It first makes the sine and cosine of every (token, pair), one per thread, and then every (token, head,
-// pair group) turns with them, so the angle of a pair is computed once however many heads share it.  The angle is exact: turns per
+// pair group) turns with them, so the angle of a pair is computed once however many heads share it.  Nothing is lost at far positions: turns per
 // position are a 64-bit fraction, and position * fraction wraps modulo 2^64 exactly where the angle wraps modulo one turn, so
-// the upper bits are the angle in [-1/2, 1/2) turns whatever the position.  The heads' elements are requested ahead of that, so that
+// the upper bits are the angle in [-1/2, 1/2) turns (off by what the fraction was rounded by times the position, 2^-29 of a turn at most).  The heads' elements are requested ahead of that, so that
 // the arithmetic of the angles runs under the loads.  HBM bounds it: one read and one write of the heads, 8,191 tokens of 28 + 4 heads
 // of 128 24 us (5.5 TB/s), 32,768 97 us; a block of six tokens is a launch, 2.9 us.
 #include <math.h>

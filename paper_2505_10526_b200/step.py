@@ -28,7 +28,7 @@ class VerifyStep:
                  rope=None, n_groups=0, rules=False):
         """``rope``: None, or the keyword arguments of ``rope_desc`` from ``rot_dim`` on together with ``turns``
         (massv_rope_frequencies); the step's inputs may then hold ``pos_delta`` (int32 [B]).
-        ``n_groups`` > 0: the inputs hold ``group_start`` and ``shared_lens``.
+        ``n_groups`` > 0: the inputs hold ``group_start`` and ``shared_lens``; ``attn_kernel`` and ``kv_chunk`` are not used then.
         ``rules``: the inputs hold ``rules`` (``logit_rules``), and ``run`` adds the emitted tokens to the history that they read, or to
         ``output_bits`` and ``counts`` of the inputs where these are given."""
         self.device = torch.device(device)
@@ -40,7 +40,8 @@ class VerifyStep:
         dev = self.device
         self.n_groups, self.rules, self.vocab = n_groups, bool(rules), vocab
         if n_groups and mv.massv_verify_attn_shared_workspace_size(self.adesc, n_groups) == 0:
-            raise ValueError("massv: groups that share a prefix take no window, at most 256 groups and 2,048 sequences")
+            raise ValueError("massv: groups that share a prefix take no window, at most 256 groups and 2,048 sequences, and no more blocks than massv_verify_attn_shared counts "
+                             "(include/massv.h)")
         self.attn_ws = mv.alloc_workspace(mv.massv_verify_attn_shared_workspace_size(self.adesc, n_groups) if n_groups
                                           else mv.massv_verify_attn_workspace_size(self.adesc), dev)
         self.accept_ws = mv.alloc_workspace(mv.massv_accept_logits_workspace_size(self.cdesc) if rules
